@@ -194,6 +194,56 @@ int emoe_router_topk(emoe_ctx* ctx, const void* x, int act_dtype, int T, int d, 
 int emoe_permute(emoe_ctx* ctx, const int32_t* ids, int n_pairs, int E, int32_t* out_counts, int32_t* out_off,
                  int32_t* out_perm, int32_t* out_slot_of_pair, void* stream);
 
+/* ---- rows in expert order, and back: training the layer, or multiplying its experts yourself ------------------
+ * Sections 1 and 2.1 describe the layer as router, experts and gate-weighted sum; emoe_moe_forward runs all of it on packed
+ * experts.  These calls give the steps around the experts on tensors of the caller, with their gradients, for programs
+ * whose experts (or adapters beside them, emoe_lowrank_*) are not packed yet.  With p = t*top_k + j a (token, pick) pair and s(p)
+ * its place in the stable order by expert (emoe_permute):
+ *   emoe_dispatch           rows[s(p)] = w[p] * x[t]
+ *   emoe_dispatch_backward  dx[t] = sum_j w[p] * drows[s(p)],   dweights[p] = sum_i x[t][i] * drows[s(p)][i]
+ *   emoe_combine            y[t] = sum_j gates[p] * rows[s(p)]
+ *   emoe_combine_backward   drows[s(p)] = gates[p] * dy[t],     dgates[p] = sum_i rows[s(p)][i] * dy[t][i]
+ * Sums and products are fp32, j ascending, each result is rounded once; the same inputs give the same bits.  Any d; rows
+ * whose length, strides and addresses are multiples of 16 bytes are several times faster.  Tensors may be further apart
+ * than d (the strides below); buffers of one call must not overlap, but drows may be `rows` itself.
+ * Pairs whose slot is outside [0, T*top_k) (a dropped pair has -1) take no part: their weight's gradient is 0, and rows that no pair
+ * owns are neither read nor written.  These calls use no workspace: calls on different streams may overlap (a bad id sets the
+ * context's one check word). */
+typedef struct emoe_dispatch_desc {
+  int32_t d;            /* values per row */
+  int32_t n_experts;    /* 1 .. EMOE_MAX_EXPERTS */
+  int32_t top_k;        /* 1 .. EMOE_MAX_TOP_K */
+  int32_t token_dtype;  /* EMOE_DTYPE_F32 | EMOE_DTYPE_BF16: x, dx, y, dy */
+  int32_t row_dtype;    /* EMOE_DTYPE_F32 | EMOE_DTYPE_BF16: rows, drows */
+  int32_t reserved;
+  int64_t token_stride; /* values between the starts of two tokens; 0 = d */
+  int64_t row_stride;   /* values between the starts of two rows; 0 = d */
+} emoe_dispatch_desc;
+
+/* ids [T][top_k]; weights NULL (1) or [T][top_k] fp32; out_counts [E], out_off [E+1], out_perm and out_slot_of_pair [T*top_k] as
+ * emoe_permute writes them; out_rows [T*top_k][d].  Ids outside [0,E) set the device check word and are dropped. */
+int emoe_dispatch(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* x, int T, const int32_t* ids, const float* weights,
+                  int32_t* out_counts, int32_t* out_off, int32_t* out_perm, int32_t* out_slot_of_pair, void* out_rows, void* stream);
+/* dweights NULL or [T][top_k] fp32 (then x is needed). */
+int emoe_dispatch_backward(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* drows, int T, const int32_t* slot_of_pair,
+                           const float* weights, const void* x, void* dx, float* dweights, void* stream);
+/* gates NULL (1) or [T][top_k] fp32. */
+int emoe_combine(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* rows, int T, const int32_t* slot_of_pair, const float* gates, void* y,
+                 void* stream);
+/* dgates NULL or [T][top_k] fp32 (then rows are needed). */
+int emoe_combine_backward(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* dy, int T, const int32_t* slot_of_pair, const float* gates,
+                          const void* rows, void* drows, float* dgates, void* stream);
+
+/* Gradient of the router's logits from the gradient of its Top-K gates (emoe_router_topk; the picks themselves are constants).
+ *   EMOE_GATE_SOFTMAX:        dlogits_e = p_e * (D_e - sum_e' p_e' D_e'),  p = softmax(logits), D_e = sum of dgates over the picks of e
+ *   EMOE_GATE_SOFTMAX_RENORM: dlogits_e = sum over the picks j of e of g_j * (dgates_j - sum_m g_m dgates_m), g = softmax over the
+ *                             picked logits; 0 for experts that are no pick
+ * logits [T][E] as emoe_router_topk writes them (bias included), ids and dgates [T][top_k], dlogits [T][E] fp32 (not in place).  Picks outside
+ * [0,E) set the device check word and take no part; a token whose (picked) logits are all -inf gets zeros.  The products that follow,
+ * dx += dlogits W^T and dW = x^T dlogits, are plain matrix products. */
+int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const int32_t* ids, const float* dgates, int top_k, int gate_mode,
+                       float* dlogits, void* stream);
+
 /* ---- the layer ------------------------------------------------------------------------ */
 
 /* Full layer forward (Sections 1, 2.1 on the Section 3.2 storage):

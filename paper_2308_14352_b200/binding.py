@@ -43,6 +43,7 @@ EXPORTS = (
     "emoe_cached_layer", "emoe_cache_slot_of", "emoe_cache_get_stats", "emoe_cache_set_timing", "emoe_last_expert_counts", "emoe_policy_create", "emoe_policy_destroy", "emoe_policy_register",
     "emoe_policy_prefetch", "emoe_policy_acquire", "emoe_policy_release", "emoe_policy_get_stats", "emoe_rank_experts",
     "emoe_build_profile2", "emoe_rank_experts2",
+    "emoe_dispatch", "emoe_dispatch_backward", "emoe_combine", "emoe_combine_backward", "emoe_gate_backward",
 )
 
 
@@ -60,6 +61,11 @@ class emoe_expert(ctypes.Structure):
 class emoe_layer_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("d_model", "d_ff", "n_experts", "top_k", "act", "gate_mode", "group", "scale_dtype", "act_dtype")]
+
+
+class emoe_dispatch_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("d", "n_experts", "top_k", "token_dtype", "row_dtype", "reserved")] + \
+               [("token_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
 
 
 class emoe_cache_stats(ctypes.Structure):
@@ -145,6 +151,12 @@ def lib() -> ctypes.CDLL:
         L.emoe_moe_forward_routed_static.argtypes = [i32, ctypes.POINTER(emoe_layer_desc), vp, i32, vp, vp,
                                                      ctypes.POINTER(emoe_expert), vp, vp]
         L.emoe_static_device_status.argtypes = [i32, vp]
+        pd = ctypes.POINTER(emoe_dispatch_desc)
+        L.emoe_dispatch.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.emoe_dispatch_backward.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.emoe_combine.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp]
+        L.emoe_combine_backward.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.emoe_gate_backward.argtypes = [vp, vp, i32, i32, vp, vp, i32, i32, vp, vp]
         L.emoe_read_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_float),
                                        ctypes.POINTER(ctypes.c_int)]
         _lib = L
@@ -459,3 +471,27 @@ def emoe_rank_experts2(prior2_layer, prev2_ids, prev1_ids):
     _check(lib().emoe_rank_experts2(tab.ctypes.data_as(ctypes.POINTER(ctypes.c_float)), E, p2.ctypes.data_as(pi), len(p2),
                                     p1.ctypes.data_as(pi), len(p1), out.ctypes.data_as(pi)), "emoe_rank_experts2")
     return out
+
+
+def emoe_dispatch(ctx, desc: emoe_dispatch_desc, x_ptr, T, ids_ptr, weights_ptr, counts_ptr, off_ptr, perm_ptr, slot_of_pair_ptr, rows_ptr,
+                  stream=0) -> None:
+    _check(lib().emoe_dispatch(ctx, desc, x_ptr, T, ids_ptr, weights_ptr, counts_ptr, off_ptr, perm_ptr, slot_of_pair_ptr, rows_ptr, stream),
+           "emoe_dispatch")
+
+
+def emoe_dispatch_backward(ctx, desc: emoe_dispatch_desc, drows_ptr, T, slot_of_pair_ptr, weights_ptr, x_ptr, dx_ptr, dweights_ptr, stream=0) -> None:
+    _check(lib().emoe_dispatch_backward(ctx, desc, drows_ptr, T, slot_of_pair_ptr, weights_ptr, x_ptr, dx_ptr, dweights_ptr, stream),
+           "emoe_dispatch_backward")
+
+
+def emoe_combine(ctx, desc: emoe_dispatch_desc, rows_ptr, T, slot_of_pair_ptr, gates_ptr, y_ptr, stream=0) -> None:
+    _check(lib().emoe_combine(ctx, desc, rows_ptr, T, slot_of_pair_ptr, gates_ptr, y_ptr, stream), "emoe_combine")
+
+
+def emoe_combine_backward(ctx, desc: emoe_dispatch_desc, dy_ptr, T, slot_of_pair_ptr, gates_ptr, rows_ptr, drows_ptr, dgates_ptr, stream=0) -> None:
+    _check(lib().emoe_combine_backward(ctx, desc, dy_ptr, T, slot_of_pair_ptr, gates_ptr, rows_ptr, drows_ptr, dgates_ptr, stream),
+           "emoe_combine_backward")
+
+
+def emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream=0) -> None:
+    _check(lib().emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream), "emoe_gate_backward")

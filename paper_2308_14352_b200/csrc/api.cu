@@ -575,6 +575,11 @@ ExpertCache*& ctx_cache(emoe_ctx* ctx) { return ctx->cache; }
 int ctx_device(const emoe_ctx* ctx) { return ctx->device; }
 bool ctx_dependent_launch(const emoe_ctx* ctx) { return ctx->pdl && !ctx->timing; }
 int ctx_cuda_fail(emoe_ctx* ctx, cudaError_t e) { return cuda_fail(ctx, e); }
+int* ctx_check_word(emoe_ctx* ctx) { return ctx->check_word; }
+char* ctx_workspace(emoe_ctx* ctx, size_t* bytes) {
+  *bytes = ctx->workspace_bytes;
+  return ctx->workspace;
+}
 }  // namespace emoe
 
 extern "C" {
