@@ -72,6 +72,7 @@ extern "C" {
 
 #define EMOE_MAX_EXPERTS 256
 #define EMOE_MAX_TOP_K 8
+#define EMOE_MAX_RANK 64
 
 typedef struct emoe_ctx emoe_ctx;
 
@@ -243,6 +244,49 @@ int emoe_combine_backward(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const v
  * dx += dlogits W^T and dW = x^T dlogits, are plain matrix products. */
 int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const int32_t* ids, const float* dgates, int top_k, int gate_mode,
                        float* dlogits, void* stream);
+
+/* ---- low-rank adapters beside a shared projection ------------------------------------------------------------
+ * The packed weights of an expert or of a shared projection stay as they are (Section 3.2); what a request, a task or a round
+ * of training adds to them is a low-rank term per adapter a, with factors A_a [rank][in_dim] and B_a [out_dim][rank] and a
+ * scale s_a.  Row i of a call belongs to adapter a(i):
+ *   emoe_lowrank_forward   v_i = A_a x_i,           y_i  = base_i + s_a * B_a v_i
+ *   emoe_lowrank_backward  dv_i = s_a * B_a^T dy_i, dx_i = dx_base_i + A_a^T dv_i,
+ *                          dA_a = sum_i dv_i x_i^T, dB_a = s_a * sum_i dy_i v_i^T
+ * base is the shared projection's output (dx_base the gradient that came through it); it may be y (dx) itself, or NULL for 0.
+ * Which rows are whose: `ids` [n], one adapter per row in any order (a batch of requests; -1: none), or `off` [n_adapters + 1], rows
+ * off[a] .. off[a+1]-1 belong to a (rows sorted by expert: the offsets of emoe_dispatch; ascending, off[n_adapters] <= n).  Exactly
+ * one of the two is given.
+ * Rows of no adapter: with ids y = base and v = 0 (nothing is touched where y is base), with off they are left as they were; they
+ * take no part in dA and dB.  An id other than -1 outside [0,n_adapters) counts as -1 and sets the device check word.
+ * Sums are fp32 or better; bf16 results are rounded once, fp32 tensors are multiplied with all their 24 bits (an infinite value in
+ * them gives NaN); the same inputs give the same bits.
+ * Limits: rank 1 .. EMOE_MAX_RANK (any; multiples of 8 are faster), in_dim and out_dim multiples of 8, strides multiples of 16 bytes, tensors
+ * 16-byte aligned. */
+typedef struct emoe_lowrank_desc {
+  int32_t n_adapters; /* 1 .. EMOE_MAX_EXPERTS */
+  int32_t rank;
+  int32_t in_dim;
+  int32_t out_dim;
+  int32_t dtype;      /* EMOE_DTYPE_F32 | EMOE_DTYPE_BF16: x, base, y, A, B and the gradients of rows */
+  int32_t reserved;
+  int64_t x_stride;   /* values between the starts of two rows of x, dx and dx_base; 0 = in_dim */
+  int64_t y_stride;   /* ... of y, base and dy; 0 = out_dim */
+} emoe_lowrank_desc;
+
+/* Context workspace that calls of at most n rows need (0 for an invalid description): pass the maximum over what the context
+ * serves to emoe_create.  Forward calls with `off`, or of at most 512 rows, use none. */
+size_t emoe_lowrank_workspace_bytes(const emoe_lowrank_desc* desc, int n);
+
+/* A [n_adapters][rank][in_dim], B [n_adapters][out_dim][rank]; scales NULL (1) or [n_adapters] fp32; x [n][in_dim]; y [n][out_dim];
+ * out_v NULL or [n][rank] fp32: the v_i that the backward pass needs.  No buffer that is written overlaps another, but y may be base. */
+int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const void* A, const void* B, const float* scales, const void* x, int n,
+                         const int32_t* ids, const int32_t* off, const void* base, void* y, float* out_v, void* stream);
+
+/* dx [n][in_dim] (NULL: not wanted), dA [n_adapters][rank][in_dim] and dB [n_adapters][out_dim][rank] fp32 (each NULL: not wanted),
+ * written whole: zeros for adapters without rows.  dx needs A and B, dA needs B and x, dB needs v. */
+int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const void* A, const void* B, const float* scales, const void* x,
+                          const void* dy, int n, const int32_t* ids, const int32_t* off, const float* v, const void* dx_base, void* dx, float* dA,
+                          float* dB, void* stream);
 
 /* ---- the layer ------------------------------------------------------------------------ */
 

@@ -44,6 +44,7 @@ EXPORTS = (
     "emoe_policy_prefetch", "emoe_policy_acquire", "emoe_policy_release", "emoe_policy_get_stats", "emoe_rank_experts",
     "emoe_build_profile2", "emoe_rank_experts2",
     "emoe_dispatch", "emoe_dispatch_backward", "emoe_combine", "emoe_combine_backward", "emoe_gate_backward",
+    "emoe_lowrank_workspace_bytes", "emoe_lowrank_forward", "emoe_lowrank_backward",
 )
 
 
@@ -66,6 +67,11 @@ class emoe_layer_desc(ctypes.Structure):
 class emoe_dispatch_desc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("d", "n_experts", "top_k", "token_dtype", "row_dtype", "reserved")] + \
                [("token_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class emoe_lowrank_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_adapters", "rank", "in_dim", "out_dim", "dtype", "reserved")] + \
+               [("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64)]
 
 
 class emoe_cache_stats(ctypes.Structure):
@@ -156,6 +162,11 @@ def lib() -> ctypes.CDLL:
         L.emoe_dispatch_backward.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp]
         L.emoe_combine.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp]
         L.emoe_combine_backward.argtypes = [vp, pd, vp, i32, vp, vp, vp, vp, vp, vp]
+        pl = ctypes.POINTER(emoe_lowrank_desc)
+        L.emoe_lowrank_workspace_bytes.restype = sz
+        L.emoe_lowrank_workspace_bytes.argtypes = [pl, i32]
+        L.emoe_lowrank_forward.argtypes = [vp, pl, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.emoe_lowrank_backward.argtypes = [vp, pl, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.emoe_gate_backward.argtypes = [vp, vp, i32, i32, vp, vp, i32, i32, vp, vp]
         L.emoe_read_timing.argtypes = [vp, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_float),
                                        ctypes.POINTER(ctypes.c_int)]
@@ -495,3 +506,19 @@ def emoe_combine_backward(ctx, desc: emoe_dispatch_desc, dy_ptr, T, slot_of_pair
 
 def emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream=0) -> None:
     _check(lib().emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream), "emoe_gate_backward")
+
+
+def emoe_lowrank_workspace_bytes(desc: emoe_lowrank_desc, n: int) -> int:
+    return int(lib().emoe_lowrank_workspace_bytes(desc, n))
+
+
+def emoe_lowrank_forward(ctx, desc: emoe_lowrank_desc, A_ptr, B_ptr, scales_ptr, x_ptr, n, ids_ptr, off_ptr, base_ptr, y_ptr, out_v_ptr,
+                         stream=0) -> None:
+    _check(lib().emoe_lowrank_forward(ctx, desc, A_ptr, B_ptr, scales_ptr, x_ptr, n, ids_ptr, off_ptr, base_ptr, y_ptr, out_v_ptr, stream),
+           "emoe_lowrank_forward")
+
+
+def emoe_lowrank_backward(ctx, desc: emoe_lowrank_desc, A_ptr, B_ptr, scales_ptr, x_ptr, dy_ptr, n, ids_ptr, off_ptr, v_ptr, dx_base_ptr, dx_ptr,
+                          dA_ptr, dB_ptr, stream=0) -> None:
+    _check(lib().emoe_lowrank_backward(ctx, desc, A_ptr, B_ptr, scales_ptr, x_ptr, dy_ptr, n, ids_ptr, off_ptr, v_ptr, dx_base_ptr, dx_ptr,
+                                       dA_ptr, dB_ptr, stream), "emoe_lowrank_backward")

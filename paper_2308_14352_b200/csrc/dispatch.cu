@@ -184,20 +184,21 @@ __global__ void __launch_bounds__(ROWS_THREADS) gather_kernel(RowsArgs a) {
 // Stable counting sort by one cluster of up to eight CTAs.  A warp owns a run of consecutive pairs: it counts them by expert
 // (match gives the lanes of an expert and their ranks), the counts of all warps in front of it, of its CTA and of the CTAs before (read
 // over distributed shared memory), are its first places, and a second walk hands them out.  Two cluster-wide waits,
-// no order-dependent atomics.
+// no order-dependent atomics.  keep_rest: ids outside [0, E - 1) count as E - 1.
 constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CLUSTER = 8;
 
 __global__ void __launch_bounds__(SORT_THREADS)
-    sort_pairs_kernel(const int32_t* __restrict__ ids, int n, int E, int none, int32_t* __restrict__ counts, int32_t* __restrict__ off,
+    sort_pairs_kernel(const int32_t* __restrict__ ids, int n, int E, bool keep_rest, int32_t* __restrict__ counts, int32_t* __restrict__ off,
                       int32_t* __restrict__ perm, int32_t* __restrict__ slot_of_pair, int* __restrict__ check_word) {
   extern __shared__ int first[];  // [SORT_WARPS][E]: pairs of a warp by expert, then the next place of each
-  __shared__ int hist[EMOE_MAX_EXPERTS], s_off[EMOE_MAX_EXPERTS + 1];
+  __shared__ int hist[EMOE_MAX_EXPERTS + 1], s_off[EMOE_MAX_EXPERTS + 2];
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks());
   const int run = (n + ctas * SORT_THREADS - 1) / (ctas * SORT_THREADS) * 32;
   const int begin = (rank * SORT_WARPS + warp) * run;
   int* mine = first + warp * E;
+  const int named = keep_rest ? E - 1 : E, rest = keep_rest ? E - 1 : -1;
   for (int i = tid; i < SORT_WARPS * E; i += SORT_THREADS) first[i] = 0;
   __syncthreads();
   pdl_wait();
@@ -205,10 +206,13 @@ __global__ void __launch_bounds__(SORT_THREADS)
   bool bad = false;
   for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32) {
     const int p = p0 + lane;
-    const int id = p < n ? ids[p] : none;
-    const bool ok = id >= 0 && id < E;
-    bad |= !ok && id != none;
-    const unsigned same = __match_any_sync(0xffffffffu, ok ? id : -1);
+    int id = p < n ? ids[p] : -1;
+    if (p < n && (id < 0 || id >= named)) {
+      bad |= !keep_rest || id != -1;
+      id = rest;
+    }
+    const bool ok = id >= 0;
+    const unsigned same = __match_any_sync(0xffffffffu, id);
     if (ok && lane == __ffs(same) - 1) mine[id] += __popc(same);
     __syncwarp();
   }
@@ -262,9 +266,10 @@ __global__ void __launch_bounds__(SORT_THREADS)
   __syncthreads();
   for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32) {
     const int p = p0 + lane;
-    const int id = p < n ? ids[p] : none;
-    const bool ok = id >= 0 && id < E;
-    const unsigned same = __match_any_sync(0xffffffffu, ok ? id : -1);
+    int id = p < n ? ids[p] : -1;
+    if (id >= named || id < 0) id = p < n ? rest : -1;
+    const bool ok = id >= 0;
+    const unsigned same = __match_any_sync(0xffffffffu, id);
     int pos = -1;
     if (ok) {
       pos = mine[id] + __popc(same & ((1u << lane) - 1u));
@@ -632,7 +637,7 @@ bool words_aligned(const P*... p) {
 
 }  // namespace
 
-cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, int none, int32_t* counts, int32_t* off, int32_t* perm, int32_t* slot_of_pair,
+cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32_t* counts, int32_t* off, int32_t* perm, int32_t* slot_of_pair,
                               int* check_word, cudaStream_t st) {
   const int ctas = n <= 2 * SORT_THREADS ? 1 : SORT_CLUSTER;
   cudaLaunchConfig_t cfg = {};
@@ -640,7 +645,7 @@ cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, int none, int32_
   cfg.blockDim = dim3(SORT_THREADS);
   cfg.dynamicSmemBytes = sizeof(int) * SORT_WARPS * E;
   cfg.stream = st;
-  static_assert(sizeof(int) * (SORT_WARPS + 2) * EMOE_MAX_EXPERTS + 64 <= 48 * 1024, "no larger limit is asked for");
+  static_assert(sizeof(int) * (SORT_WARPS + 2) * (EMOE_MAX_EXPERTS + 1) + 64 <= 48 * 1024, "no larger limit is asked for");
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {static_cast<unsigned>(ctas), 1, 1};
@@ -648,7 +653,7 @@ cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, int none, int32_
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = g_pdl_enabled ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, sort_pairs_kernel, ids, n, E, none, counts, off, perm, slot_of_pair, check_word);
+  return cudaLaunchKernelEx(&cfg, sort_pairs_kernel, ids, n, E, rest, counts, off, perm, slot_of_pair, check_word);
 }
 
 }  // namespace emoe
@@ -682,7 +687,7 @@ int emoe_dispatch(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* x, 
     EMOE_CALL(ctx, launch_dispatch_one(*desc, a, ids, out_counts, out_off, out_perm, out_slot_of_pair, ctx_check_word(ctx), st));
     return EMOE_OK;
   }
-  EMOE_CALL(ctx, launch_sort_pairs(ids, T * desc->top_k, desc->n_experts, desc->n_experts, out_counts, out_off, out_perm, out_slot_of_pair,
+  EMOE_CALL(ctx, launch_sort_pairs(ids, T * desc->top_k, desc->n_experts, false, out_counts, out_off, out_perm, out_slot_of_pair,
                                    ctx_check_word(ctx), st));
   EMOE_CALL(ctx, launch_spread(*desc, a, st));
   return EMOE_OK;

@@ -1,0 +1,952 @@
+// Low-rank adapters of many requests (or experts) beside a shared projection, and their gradient.  Row i of a call belongs to
+// adapter a(i) with factors A_a [rank][in], B_a [out][rank] and scale s_a:
+//   forward   v_i = A_a x_i,                       y_i  = base_i + s_a B_a v_i
+//   backward  dv_i = s_a B_a^T dy_i,               dx_i = dx_base_i + A_a^T dv_i,   dA_a = sum_i dv_i x_i^T,  dB_a = s_a sum_i dy_i v_i^T
+// The two directions are one kernel with the factors' parts exchanged (down through the factor that is read along the rows of the
+// activations, up through the other), then one kernel for the sums over the rows of an adapter.
+//
+// What bounds them is memory: with rank 16 a value of x takes part in 16 multiply-adds for two bytes.  So no tile of activations goes
+// through shared memory: mma.sync does not care which index of the reduction a lane holds as long as both operands agree, so every lane takes
+// 16 or 32 consecutive bytes of a row straight into its fragments, each byte once.
+//
+// Precision.  The tensor cores multiply bf16 exactly and add in fp32.  bf16 tensors enter as they are; an fp32 value enters as the
+// sum of bf16 parts: three (24 bits, the value itself) where the result is fp32, so that it has fp32's accuracy, two (16 bits) for the
+// low-rank vector of a bf16 result, whose own rounding is 2^-9.  Of the nine products of two values in three parts the three smallest
+// (2^-24 of the product) are left out.
+#include <cooperative_groups.h>
+
+#include "rows.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace emoe {
+namespace {
+
+constexpr int LR_THREADS = 256, LR_WARPS = LR_THREADS / 32;
+constexpr int LR_IDS_ROWS = 512;  // most rows whose adapters every CTA looks up by itself
+
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Two fp32 values as N pairs of bf16 parts, largest first.  All parts but the last are truncated: what is left is exact, so three
+// parts are the value itself.  An infinity has no rest.
+template <int N>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+    if (N == 2 && i == N - 1) {
+      const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+      part[i] = *reinterpret_cast<const uint32_t*>(&r);
+    } else {
+      part[i] = __byte_perm(ua, ub, 0x7632);
+    }
+    a = isinf(a) ? 0.f : a - __uint_as_float(ua & 0xffff0000u);
+    b = isinf(b) ? 0.f : b - __uint_as_float(ub & 0xffff0000u);
+  }
+}
+
+template <typename T>
+struct Parts {  // bf16 parts of a factor or activation, and of the fp32 vector it is multiplied with
+  static constexpr int IN = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int VEC = sizeof(T) == 4 ? 3 : 2;
+};
+
+// a . b over the kept products of their parts
+template <int PA, int PB>
+__device__ __forceinline__ void mma_parts(float (&d)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][2]) {
+#pragma unroll
+  for (int i = PA - 1; i >= 0; --i)  // smallest first
+#pragma unroll
+    for (int j = PB - 1; j >= 0; --j)
+      if (i + j < 3) mma_bf16(d, a[i], b[j][0], b[j][1]);
+}
+
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint32_t w[4];
+  load_words(p, w);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 load16_keep(const void* p) { return *reinterpret_cast<const uint4*>(p); }
+
+struct LowrankArgs {
+  const void *x, *base;  // rows in, rows added to the result (null: zeros)
+  const void *down, *up; // forward: A, B; backward: B, A
+  const float* scales;   // null: 1
+  const int32_t *ids, *off, *perm;
+  void* y;               // null: the low-rank vectors alone
+  float* v;              // null: not wanted
+  int* check_word;
+  int n, G, rank, in_dim, out_dim, segments;  // segments: G, or G + 1 with the rows of no adapter as the last
+  int skip_none;         // rows of no adapter stay as they are
+  size_t x_stride, y_stride;
+};
+
+// Which rows this cluster works on: their number and adapter (-1: none) or 0.  Rows are listed in shared memory.
+// ids: the first row of every BT rows with the same adapter leads them; off: tiles of BT rows, segment by segment.
+template <int BT>
+__device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_rows, int* s_scan, int* adapter) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (a.ids) {
+    int own = a.ids[tile];
+    if (own < 0 || own >= a.G) {
+      if (own != -1 && tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
+      own = -1;
+    }
+    *adapter = own;
+    unsigned same[LR_IDS_ROWS / LR_THREADS];
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < LR_IDS_ROWS / LR_THREADS; ++i) {
+      const int j = i * LR_THREADS + tid;
+      int id = -2;
+      if (j < a.n) {
+        id = a.ids[j];
+        if (id < 0 || id >= a.G) id = -1;
+      }
+      same[i] = __ballot_sync(0xffffffffu, id == own);
+      const int chunk = i * LR_THREADS + warp * 32;  // first row of the ballot
+      if (lane == 0) s_scan[chunk / 32] = __popc(same[i]);
+    }
+    __syncthreads();
+    // rows with this adapter in front of the tile's own row, and in front of each chunk
+    for (int c = 0; c < tile / 32; ++c) before += s_scan[c];
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < LR_IDS_ROWS / LR_THREADS; ++i) {
+      const int chunk = i * (LR_THREADS / 32) + warp;
+      int front = 0;
+      for (int c = 0; c < chunk; ++c) front += s_scan[c];
+      if (chunk == tile / 32 && lane == 0) s_scan[LR_IDS_ROWS / 32] = before + __popc(same[i] & ((1u << (tile % 32)) - 1u));
+      same[i] = (same[i] >> lane & 1u) ? front + __popc(same[i] & ((1u << lane) - 1u)) : 0xffffffffu;  // now: rank, or none
+    }
+    __syncthreads();
+    const int first = s_scan[LR_IDS_ROWS / 32];
+    if (first % BT != 0) return 0;  // led by an earlier row
+    int total = 0;
+    for (int c = 0; c < LR_IDS_ROWS / 32; ++c) total += s_scan[c];
+    count = min(BT, total - first);
+#pragma unroll
+    for (int i = 0; i < LR_IDS_ROWS / LR_THREADS; ++i) {
+      const int rank = static_cast<int>(same[i]);
+      if (rank >= first && rank < first + BT) s_rows[rank - first] = i * LR_THREADS + tid;
+    }
+    __syncthreads();
+    return count;
+  }
+  // one thread per segment: its tiles, added up
+  int begin = 0, rows = 0;
+  if (tid < a.segments) {
+    begin = min(max(a.off[tid], 0), a.n);
+    rows = min(a.off[tid + 1], a.n) - begin;
+  }
+  const int tiles = rows > 0 ? (rows + BT - 1) / BT : 0;
+  int incl = tiles;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  if (tid == 0) s_scan[LR_WARPS] = 0;
+  // (a 257th segment, the rows of no adapter beside 256 of them)
+  const int last_begin = a.segments > LR_THREADS ? min(max(a.off[LR_THREADS], 0), a.n) : 0;
+  const int last_rows = a.segments > LR_THREADS ? min(a.off[LR_THREADS + 1], a.n) - last_begin : 0;
+  __syncthreads();
+  int front = 0, all = 0;
+  for (int w = 0; w < LR_WARPS; ++w) {
+    if (w < warp) front += s_scan[w];
+    all += s_scan[w];
+  }
+  const int first = front + incl - tiles;
+  if (tile >= first && tile < first + tiles) {
+    s_scan[LR_WARPS] = min(BT, rows - (tile - first) * BT);
+    s_scan[LR_WARPS + 1] = begin + (tile - first) * BT;
+    s_scan[LR_WARPS + 2] = tid;
+  }
+  if (tid == 0 && last_rows > 0 && tile >= all && tile < all + (last_rows + BT - 1) / BT) {
+    s_scan[LR_WARPS] = min(BT, last_rows - (tile - all) * BT);
+    s_scan[LR_WARPS + 1] = last_begin + (tile - all) * BT;
+    s_scan[LR_WARPS + 2] = LR_THREADS;
+  }
+  __syncthreads();
+  const int count = s_scan[LR_WARPS], at = s_scan[LR_WARPS + 1], g = s_scan[LR_WARPS + 2];
+  if (count == 0) return 0;
+  *adapter = g < a.G ? g : -1;
+  for (int i = tid; i < count; i += LR_THREADS) s_rows[i] = a.perm ? a.perm[at + i] : at + i;
+  __syncthreads();
+  return count;
+}
+
+// RT: rank in tiles of 16; NT: rows in tiles of 8; BACK: the down factor is B ([reduction][rank]), the up factor A ([rank][out]).
+template <typename T, int RT, int NT, bool BACK>
+struct Lowrank {
+  static constexpr int BT = NT * 8, MT = (NT + 1) / 2, RP = RT * 16;
+  static constexpr int PI = Parts<T>::IN, PV = Parts<T>::VEC;
+  static constexpr int WORDS = RT * NT >= 16 || (sizeof(T) == 4 && RT * NT >= 8) ? 4 : 8;  // of a row per lane and step: 16 or 32 bytes
+  static constexpr int VALS = WORDS * 4 / static_cast<int>(sizeof(T)), STEP = VALS * 4, KS = VALS / 4;
+  static constexpr int V_STRIDE = 16 * (RT == 1 ? 1 : RT == 2 ? 3 : 5);  // bf16 values: an odd number of 32-byte pieces, no bank met twice
+  static constexpr int RED_FLOATS = LR_WARPS / 2 * RT * NT * 4 * 32, PART_FLOATS = BT * RP;
+  static constexpr size_t SMEM = sizeof(float) * (RED_FLOATS + PART_FLOATS) + 2ull * PV * MT * 16 * V_STRIDE;
+
+  // rank index of row g (half 0) or g + 8 (half 1) of tile m of the down factor's fragments
+  __device__ static __forceinline__ int rank_of(int m, int g, int half) { return BACK ? 2 * RT * g + 2 * m + half : 16 * m + g + 8 * half; }
+  // place of a rank index in the low-rank vectors: the four that lane q of step s multiplies with lie together
+  __device__ static __forceinline__ int place_of(int r) { return r % (4 * RT) / 4 * 16 + r / (4 * RT) * 4 + r % 4; }
+
+  // N values of a factor's row from `first` on, those at or beyond `end` zero
+  template <int N>
+  __device__ static __forceinline__ void load_factor(const T* row, int first, int end, bool whole, uint32_t (&w)[N * sizeof(T) / 4]) {
+    constexpr int WN = N * sizeof(T) / 4;
+#pragma unroll
+    for (int i = 0; i < WN; ++i) w[i] = 0;
+    if (whole) {
+      if (first < end) {
+        if constexpr (WN == 1) w[0] = *reinterpret_cast<const uint32_t*>(row + first);
+        else if constexpr (WN == 2) {
+          const uint2 u = *reinterpret_cast<const uint2*>(row + first);
+          w[0] = u.x; w[1] = u.y;
+        } else {
+#pragma unroll
+          for (int i = 0; i < WN; i += 4)
+            if (first + i * 4 / static_cast<int>(sizeof(T)) < end) {
+              const uint4 u = load16_keep(reinterpret_cast<const char*>(row + first) + 4 * i);
+              w[i] = u.x; w[i + 1] = u.y; w[i + 2] = u.z; w[i + 3] = u.w;
+            }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (first + i < end) {
+          if constexpr (sizeof(T) == 4) w[i] = reinterpret_cast<const uint32_t*>(row)[first + i];
+          else w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[first + i]) << (16 * (i % 2));
+        }
+    }
+  }
+};
+
+template <typename T, int RT, int NT, bool BACK>
+__global__ void __launch_bounds__(LR_THREADS, RT * NT <= 8 && sizeof(T) == 2 ? 2 : 1) lowrank_kernel(LowrankArgs a) {
+  using L = Lowrank<T, RT, NT, BACK>;
+  constexpr int BT = L::BT, RP = L::RP, PI = L::PI, PV = L::PV, WORDS = L::WORDS, KS = L::KS;
+  extern __shared__ __align__(16) char smem[];
+  float* s_red = reinterpret_cast<float*>(smem);
+  float* s_part = s_red + L::RED_FLOATS;
+  __nv_bfloat16* s_v = reinterpret_cast<__nv_bfloat16*>(s_part + L::PART_FLOATS);
+  __shared__ int s_rows[BT], s_scan[LR_IDS_ROWS / 32 + 1];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  const int ctas = static_cast<int>(cluster.num_blocks()), cta = static_cast<int>(cluster.block_rank());
+  pdl_wait();
+  pdl_trigger();
+  int adapter = -1;
+  const int count = find_rows<BT>(a, blockIdx.x / ctas, s_rows, s_scan, &adapter);
+  if (count == 0 || (adapter < 0 && a.skip_none && !a.v)) return;  // the whole cluster
+  const T* down = static_cast<const T*>(a.down) + static_cast<size_t>(adapter < 0 ? 0 : adapter) * a.rank * a.in_dim;
+  const T* up = static_cast<const T*>(a.up) + static_cast<size_t>(adapter < 0 ? 0 : adapter) * a.rank * a.out_dim;
+
+  // ---- down: v = A x (forward), B^T dy (backward); every warp of the cluster takes a share of the reduction
+  if (adapter >= 0) {
+    float acc[RT][NT][4] = {};
+    const T* row[NT];
+    bool live[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      live[t] = t * 8 + g < count;
+      row[t] = static_cast<const T*>(a.x) + static_cast<size_t>(live[t] ? s_rows[t * 8 + g] : 0) * a.x_stride;
+    }
+    const bool whole = a.rank % (2 * RT) == 0;  // (backward) a lane's run of ranks is one aligned word of each row
+    const int steps = (a.in_dim + L::STEP - 1) / L::STEP;
+    for (int step = cta * LR_WARPS + warp; step < steps; step += ctas * LR_WARPS) {
+      const int k = step * L::STEP + q * L::VALS;  // this lane's first index of the reduction
+      uint32_t xw[NT][WORDS];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < WORDS; i += 4) {
+          uint4 u = make_uint4(0, 0, 0, 0);
+          const int at = k + i * 4 / static_cast<int>(sizeof(T));
+          if (live[t] && at < a.in_dim) u = load16(row[t] + at);
+          xw[t][i] = u.x; xw[t][i + 1] = u.y; xw[t][i + 2] = u.z; xw[t][i + 3] = u.w;
+        }
+      uint32_t fw[BACK ? 1 : RT][2][BACK ? 1 : WORDS];
+      if constexpr (!BACK) {
+#pragma unroll
+        for (int m = 0; m < RT; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = L::rank_of(m, g, h);
+#pragma unroll
+            for (int i = 0; i < WORDS; i += 4) {
+              uint4 u = make_uint4(0, 0, 0, 0);
+              const int at = k + i * 4 / static_cast<int>(sizeof(T));
+              if (r < a.rank && at < a.in_dim) u = load16_keep(down + static_cast<size_t>(r) * a.in_dim + at);
+              fw[m][h][i] = u.x; fw[m][h][i + 1] = u.y; fw[m][h][i + 2] = u.z; fw[m][h][i + 3] = u.w;
+            }
+          }
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        uint32_t af[RT][PI][4];
+        if constexpr (!BACK) {
+#pragma unroll
+          for (int m = 0; m < RT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if constexpr (sizeof(T) == 2) {
+                af[m][0][h] = fw[m][h][2 * s];
+                af[m][0][2 + h] = fw[m][h][2 * s + 1];
+              } else {
+                uint32_t p[PI];
+                split_pair<PI>(__uint_as_float(fw[m][h][4 * s]), __uint_as_float(fw[m][h][4 * s + 1]), p);
+#pragma unroll
+                for (int i = 0; i < PI; ++i) af[m][i][h] = p[i];
+                split_pair<PI>(__uint_as_float(fw[m][h][4 * s + 2]), __uint_as_float(fw[m][h][4 * s + 3]), p);
+#pragma unroll
+                for (int i = 0; i < PI; ++i) af[m][i][2 + h] = p[i];
+              }
+            }
+        } else {
+          // four rows of B, of each the ranks 2 RT g ..: pairs of rows are interleaved into fragments
+          constexpr int WN = 2 * RT * static_cast<int>(sizeof(T)) / 4;
+          uint32_t w[4][WN];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int at = k + 4 * s + i;
+            L::template load_factor<2 * RT>(down + static_cast<size_t>(at) * a.rank, 2 * RT * g, at < a.in_dim ? a.rank : 0, whole, w[i]);
+          }
+#pragma unroll
+          for (int m = 0; m < RT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {  // rows 0 and 1, rows 2 and 3
+                if constexpr (sizeof(T) == 2) {
+                  af[m][0][2 * half + h] = __byte_perm(w[2 * half][m], w[2 * half + 1][m], h ? 0x7632 : 0x5410);
+                } else {
+                  uint32_t p[PI];
+                  split_pair<PI>(__uint_as_float(w[2 * half][2 * m + h]), __uint_as_float(w[2 * half + 1][2 * m + h]), p);
+#pragma unroll
+                  for (int i = 0; i < PI; ++i) af[m][i][2 * half + h] = p[i];
+                }
+              }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          uint32_t bf[PI][2];
+          if constexpr (sizeof(T) == 2) {
+            bf[0][0] = xw[t][2 * s];
+            bf[0][1] = xw[t][2 * s + 1];
+          } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t p[PI];
+              split_pair<PI>(__uint_as_float(xw[t][4 * s + 2 * half]), __uint_as_float(xw[t][4 * s + 2 * half + 1]), p);
+#pragma unroll
+              for (int i = 0; i < PI; ++i) bf[i][half] = p[i];
+            }
+          }
+#pragma unroll
+          for (int m = 0; m < RT; ++m) mma_parts<PI, PI>(acc[m][t], af[m], bf);
+        }
+      }
+    }
+    // the warps' shares, added pairwise in a fixed order
+#pragma unroll
+    for (int half = LR_WARPS / 2; half >= 1; half >>= 1) {
+      float* slot = s_red + (warp & (half - 1)) * (RT * NT * 4 * 32) + lane;
+      if (warp >= half && warp < 2 * half) {
+#pragma unroll
+        for (int i = 0; i < RT * NT * 4; ++i) slot[i * 32] = (&acc[0][0][0])[i];
+      }
+      __syncthreads();
+      if (warp < half) {
+#pragma unroll
+        for (int i = 0; i < RT * NT * 4; ++i) (&acc[0][0][0])[i] += slot[i * 32];
+      }
+      __syncthreads();
+    }
+    if (warp == 0) {
+#pragma unroll
+      for (int m = 0; m < RT; ++m)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s_part[(t * 8 + 2 * q + i % 2) * RP + L::rank_of(m, g, i / 2)] = acc[m][t][i];
+    }
+  }
+  if (ctas > 1) cluster.sync();
+  else __syncthreads();
+
+  // ---- the vectors whole, scaled, in bf16 parts
+  const float scale = a.scales && adapter >= 0 ? a.scales[adapter] : 1.f;
+  for (int i = tid; i < L::MT * 16 * RP; i += LR_THREADS) {
+    const int t = i / RP, r = i % RP;
+    float v = 0.f;
+    if (t < BT && adapter >= 0)
+      for (int c = 0; c < ctas; ++c) v += ctas > 1 ? cluster.map_shared_rank(s_part, c)[t * RP + r] : s_part[t * RP + r];
+    const float scaled = scale * v;
+    if (a.v && t < count && r < a.rank && t % ctas == cta) a.v[static_cast<size_t>(s_rows[t]) * a.rank + r] = BACK ? scaled : v;
+    uint32_t p[PV];
+    split_pair<PV>(scaled, 0.f, p);
+#pragma unroll
+    for (int j = 0; j < PV; ++j)
+      s_v[(j * L::MT * 16 + t) * L::V_STRIDE + L::place_of(r)] = __ushort_as_bfloat16(static_cast<unsigned short>(p[j] & 0xffffu));
+  }
+  if (ctas > 1) cluster.sync();  // nobody leaves while another CTA reads its share
+  else __syncthreads();
+  if (!a.y || (adapter < 0 && a.skip_none)) return;
+
+  // ---- up: y = base + B v; a warp takes 32 channels of all rows at a time, a lane eight neighbouring ones of two rows
+  const bool whole = a.rank % (RT == 1 ? 4 : 8) == 0;  // (forward) a lane's run of ranks is whole aligned words
+  const int groups = (a.out_dim + 31) / 32;
+  for (int group = cta * LR_WARPS + warp; group < groups; group += ctas * LR_WARPS) {
+    const int n0 = group * 32, mine = n0 + 8 * q;  // the lane's channels of the result
+    uint32_t bw[L::MT][2][sizeof(T) * 2];
+#pragma unroll
+    for (int t = 0; t < L::MT; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = t * 16 + h * 8 + g;
+#pragma unroll
+        for (int w = 0; w < static_cast<int>(sizeof(T)) * 2; w += 4) {
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (a.base && i < count && mine < a.out_dim)
+            u = load16(static_cast<const T*>(a.base) + static_cast<size_t>(s_rows[i]) * a.y_stride + mine + w * 4 / static_cast<int>(sizeof(T)));
+          bw[t][h][w] = u.x; bw[t][h][w + 1] = u.y; bw[t][h][w + 2] = u.z; bw[t][h][w + 3] = u.w;
+        }
+      }
+    // up factor: tile i of eight columns holds the channels 8 c' + 2 i + (c & 1), c = 2 c' + (c & 1) the column of this lane
+    uint32_t uf[RT][4][PI][2];
+    if constexpr (!BACK) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int ch = n0 + 8 * (g >> 1) + 2 * i + (g & 1);
+        constexpr int WN = 4 * RT * static_cast<int>(sizeof(T)) / 4;
+        uint32_t w[WN];
+        L::template load_factor<4 * RT>(up + static_cast<size_t>(ch) * a.rank, 4 * RT * q, ch < a.out_dim && adapter >= 0 ? a.rank : 0, whole, w);
+#pragma unroll
+        for (int s = 0; s < RT; ++s) {
+          if constexpr (sizeof(T) == 2) {
+            uf[s][i][0][0] = w[2 * s];
+            uf[s][i][0][1] = w[2 * s + 1];
+          } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              uint32_t p[PI];
+              split_pair<PI>(__uint_as_float(w[4 * s + 2 * half]), __uint_as_float(w[4 * s + 2 * half + 1]), p);
+#pragma unroll
+              for (int j = 0; j < PI; ++j) uf[s][i][j][half] = p[j];
+            }
+          }
+        }
+      }
+    } else {
+      const int ch = n0 + 8 * (g >> 1);
+#pragma unroll
+      for (int s = 0; s < RT; ++s)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t w[2][sizeof(T) * 2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = 4 * RT * q + 4 * s + 2 * half + j;
+            L::template load_factor<8>(up + static_cast<size_t>(r) * a.out_dim, ch, r < a.rank && adapter >= 0 ? a.out_dim : 0, true, w[j]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 2) {
+              uf[s][i][0][half] = __byte_perm(w[0][i], w[1][i], (g & 1) ? 0x7632 : 0x5410);
+            } else {
+              uint32_t p[PI];
+              const bool odd = g & 1;
+              split_pair<PI>(__uint_as_float(odd ? w[0][2 * i + 1] : w[0][2 * i]), __uint_as_float(odd ? w[1][2 * i + 1] : w[1][2 * i]), p);
+#pragma unroll
+              for (int j = 0; j < PI; ++j) uf[s][i][j][half] = p[j];
+            }
+          }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < L::MT; ++t) {
+      float d[4][4] = {};
+#pragma unroll
+      for (int s = 0; s < RT; ++s) {
+        uint32_t vf[PV][4];
+#pragma unroll
+        for (int j = 0; j < PV; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint2 u = *reinterpret_cast<const uint2*>(s_v + (j * L::MT * 16 + t * 16 + h * 8 + g) * L::V_STRIDE + s * 16 + 4 * q);
+            vf[j][h] = u.x;
+            vf[j][2 + h] = u.y;
+          }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma_parts<PV, PI>(d[i], vf, uf[s][i]);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int i = t * 16 + h * 8 + g;
+        if (i >= count || mine >= a.out_dim) continue;
+        Piece<T, 8> p;
+#pragma unroll
+        for (int w = 0; w < Piece<T, 8>::WORDS; ++w) p.w[w] = bw[t][h][w];
+        float f[8];
+        widen<T, 8>(p, f);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          f[2 * c] += d[c][2 * h];
+          f[2 * c + 1] += d[c][2 * h + 1];
+        }
+        store_piece<T, 8>(static_cast<T*>(a.y) + static_cast<size_t>(s_rows[i]) * a.y_stride + mine, narrow<T, 8>(f));
+      }
+    }
+  }
+}
+
+// ---- gradients of the factors -------------------------------------------------------------------
+
+// out[c][r] = sum over an adapter's rows of act[row][c] vec[row][r]:  dB from dy and s v (out [N][rank]), dA from x and dv (out [rank][K]).
+// The reduction runs over rows, so a lane takes the same eight channels of four rows and interleaves pairs of rows.  A CTA owns a chunk
+// of an adapter's rows and 64 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
+// parts.  An adapter whose rows are one chunk is written at once, else its chunks' shares are joined behind this kernel in order.
+constexpr int GR_ROWS = 64, GR_CHANNELS = 64 * LR_WARPS;
+
+struct GradArgs {
+  const void* act[2];     // dy, x
+  const float* vec[2];    // v, dv
+  size_t stride[2];
+  int dim[2];             // out_dim, in_dim
+  float* out[2];          // dB, dA (null: not wanted)
+  const float* scales;    // of dB
+  const int32_t *off, *perm;
+  float* part[2];         // [chunks of adapters with several][dim][rank]
+  int* check_word;
+  int n, G, rank, chunk_rows, blocks[2], places;
+};
+
+// Chunk `c` of the list of all adapters' chunks: adapter, first row and rows, number of its adapter's chunks and its place among the chunks of
+// adapters with several; false: no such chunk.  Every thread calls it.
+struct Chunk {
+  int adapter, begin, rows, of_adapter, place;
+};
+__device__ __forceinline__ bool find_chunk(const GradArgs& a, int c, int* s_scan, Chunk* out) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int begin = 0, rows = 0;
+  if (tid < a.G) {
+    begin = min(max(a.off[tid], 0), a.n);
+    rows = max(min(a.off[tid + 1], a.n) - begin, 0);
+  }
+  const int chunks = (rows + a.chunk_rows - 1) / a.chunk_rows, several = chunks > 1 ? chunks : 0;
+  int i0 = chunks, i1 = several;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u0 = __shfl_up_sync(0xffffffffu, i0, o), u1 = __shfl_up_sync(0xffffffffu, i1, o);
+    if (lane >= o) {
+      i0 += u0;
+      i1 += u1;
+    }
+  }
+  if (lane == 31) {
+    s_scan[warp] = i0;
+    s_scan[LR_WARPS + warp] = i1;
+  }
+  if (tid == 0) s_scan[2 * LR_WARPS] = -1;
+  __syncthreads();
+  int f0 = i0 - chunks, f1 = i1 - several;
+  for (int w = 0; w < warp; ++w) {
+    f0 += s_scan[w];
+    f1 += s_scan[LR_WARPS + w];
+  }
+  if (c >= f0 && c < f0 + chunks) {
+    s_scan[2 * LR_WARPS] = tid;
+    s_scan[2 * LR_WARPS + 1] = begin + (c - f0) * a.chunk_rows;
+    s_scan[2 * LR_WARPS + 2] = min(a.chunk_rows, rows - (c - f0) * a.chunk_rows);
+    s_scan[2 * LR_WARPS + 3] = chunks;
+    s_scan[2 * LR_WARPS + 4] = f1 + (c - f0);
+  }
+  __syncthreads();
+  const int* s = s_scan + 2 * LR_WARPS;
+  *out = {s[0], s[1], s[2], s[3], s[4]};
+  return s[0] >= 0;
+}
+
+template <typename T, int RT>
+__global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a) {
+  constexpr int NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
+  __shared__ uint32_t s_vec[3][PAIRS][W_STRIDE];
+  __shared__ int s_rows[GR_ROWS], s_scan[2 * LR_WARPS + 5];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  pdl_wait();
+  pdl_trigger();
+  Chunk ch;
+  if (!find_chunk(a, blockIdx.x, s_scan, &ch)) return;
+  if (ch.of_adapter > 1 && ch.place >= a.places) {  // only where the segments overlap
+    if (tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
+    return;
+  }
+  const int which = static_cast<int>(blockIdx.y) >= a.blocks[0], block = blockIdx.y - (which ? a.blocks[0] : 0);
+  const int dim = a.dim[which], c0 = block * GR_CHANNELS + warp * 64 + 8 * g;  // this lane's eight channels
+  const T* act = static_cast<const T*>(a.act[which]);
+  const float* vec = a.vec[which];
+  const float scale = which == 0 && a.scales ? a.scales[ch.adapter] : 1.f;
+  float acc[4][NR][4] = {};
+  for (int r0 = 0; r0 < ch.rows; r0 += GR_ROWS) {
+    const int rows = min(GR_ROWS, ch.rows - r0);
+    __syncthreads();  // the vectors of the rows before have been used
+    for (int i = tid; i < GR_ROWS; i += LR_THREADS)
+      s_rows[i] = i < rows ? (a.perm ? a.perm[ch.begin + r0 + i] : ch.begin + r0 + i) : -1;
+    __syncthreads();
+    for (int i = tid; i < PAIRS * RP; i += LR_THREADS) {
+      const int pair = i / RP, r = i % RP, ra = s_rows[2 * pair], rb = s_rows[2 * pair + 1];
+      const float va = ra >= 0 && r < a.rank ? scale * vec[static_cast<size_t>(ra) * a.rank + r] : 0.f;
+      const float vb = rb >= 0 && r < a.rank ? scale * vec[static_cast<size_t>(rb) * a.rank + r] : 0.f;
+      uint32_t p[3];
+      split_pair<3>(va, vb, p);
+#pragma unroll
+      for (int j = 0; j < 3; ++j) s_vec[j][pair][r] = p[j];
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int k = 0; k < GR_ROWS; k += 16) {
+      if (k >= rows) break;
+      uint32_t w[4][sizeof(T) * 2];  // eight channels of rows 4 q .. 4 q + 3
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = s_rows[k + 4 * q + i];
+#pragma unroll
+        for (int j = 0; j < static_cast<int>(sizeof(T)) * 2; j += 4) {
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (row >= 0 && c0 < dim) u = load16(act + static_cast<size_t>(row) * a.stride[which] + c0 + j * 4 / static_cast<int>(sizeof(T)));
+          w[i][j] = u.x; w[i][j + 1] = u.y; w[i][j + 2] = u.z; w[i][j + 3] = u.w;
+        }
+      }
+      uint32_t af[4][PI][4];  // tile m: channels c0 + 2 m (rows g) and c0 + 2 m + 1 (rows g + 8)
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            if constexpr (sizeof(T) == 2) {
+              af[m][0][2 * half + h] = __byte_perm(w[2 * half][m], w[2 * half + 1][m], h ? 0x7632 : 0x5410);
+            } else {
+              uint32_t p[PI];
+              split_pair<PI>(__uint_as_float(w[2 * half][2 * m + h]), __uint_as_float(w[2 * half + 1][2 * m + h]), p);
+#pragma unroll
+              for (int j = 0; j < PI; ++j) af[m][j][2 * half + h] = p[j];
+            }
+          }
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr) {
+        uint32_t bf[3][2];
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) bf[j][half] = s_vec[j][k / 2 + 2 * q + half][nr * 8 + g];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) mma_parts<PI, 3>(acc[m][nr], af[m], bf);
+      }
+    }
+  }
+  if (c0 >= dim) return;
+  const size_t size = static_cast<size_t>(dim) * a.rank;
+  float* out = ch.of_adapter == 1 ? a.out[which] + ch.adapter * size : a.part[which] + ch.place * size;
+  // c0 + 2 m + h, rank nr * 8 + 2 q + b
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int r = nr * 8 + 2 * q + b;
+      if (r >= a.rank) continue;
+      if (which == 0) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) out[static_cast<size_t>(c0 + c) * a.rank + r] = acc[c / 2][nr][2 * (c % 2) + b];
+      } else {
+        float4* o = reinterpret_cast<float4*>(out + static_cast<size_t>(r) * dim + c0);
+        o[0] = make_float4(acc[0][nr][b], acc[0][nr][2 + b], acc[1][nr][b], acc[1][nr][2 + b]);
+        o[1] = make_float4(acc[2][nr][b], acc[2][nr][2 + b], acc[3][nr][b], acc[3][nr][2 + b]);
+      }
+    }
+}
+
+// Joins the chunks of adapters with several, in order, and clears the gradients of adapters without rows.
+__global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
+  __shared__ int s_scan[2 * LR_WARPS];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, adapter = blockIdx.x;
+  pdl_wait();
+  pdl_trigger();
+  int several = 0, chunks = 0;
+  if (tid < a.G) {
+    const int rows = max(min(a.off[tid + 1], a.n) - min(max(a.off[tid], 0), a.n), 0);
+    chunks = (rows + a.chunk_rows - 1) / a.chunk_rows;
+    several = chunks > 1 ? chunks : 0;
+  }
+  const int front = __reduce_add_sync(0xffffffffu, tid < adapter ? several : 0);
+  if (lane == 0) s_scan[warp] = front;
+  if (tid == adapter) s_scan[LR_WARPS] = chunks;
+  __syncthreads();
+  const int mine = s_scan[LR_WARPS];
+  if (mine == 1) return;
+  int place = 0;
+  for (int w = 0; w < LR_WARPS; ++w) place += s_scan[w];
+  if (place + mine > a.places && mine > 1) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (!a.out[which]) continue;
+    const size_t size = static_cast<size_t>(a.dim[which]) * a.rank;  // dim is a multiple of 8
+    float4* out = reinterpret_cast<float4*>(a.out[which] + adapter * size);
+    const float4* in = reinterpret_cast<const float4*>(a.part[which] + place * size);
+    for (size_t i = static_cast<size_t>(blockIdx.y) * LR_THREADS + tid; i < size / 4; i += static_cast<size_t>(gridDim.y) * LR_THREADS) {
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < mine; ++c) {
+        const float4 u = in[c * (size / 4) + i];
+        s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
+      }
+      out[i] = s;
+    }
+  }
+}
+
+// ---- launches -----------------------------------------------------------------------------------
+
+struct LowrankLayout {
+  size_t off, perm, dv, part[2], total;
+  int chunk_rows, chunks, places;
+};
+
+LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
+  const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  LowrankLayout w{};
+  // chunks of rows for the factors' gradients: some two CTAs per SM over both products, at least 64 rows each
+  const int blocks = (D.in_dim + GR_CHANNELS - 1) / GR_CHANNELS + (D.out_dim + GR_CHANNELS - 1) / GR_CHANNELS;
+  const int wanted = (2 * GPU_SMS + blocks - 1) / blocks, most = wanted < (n + GR_ROWS - 1) / GR_ROWS ? wanted : (n + GR_ROWS - 1) / GR_ROWS;
+  w.chunk_rows = ((n + wanted - 1) / wanted + GR_ROWS - 1) / GR_ROWS * GR_ROWS;
+  w.chunks = (n + w.chunk_rows - 1) / w.chunk_rows;  // at most `most`, which grows with n
+  // An adapter with several chunks fills all of them but one, so that there are no more than twice as many of those as all rows together make.
+  w.places = most > 1 ? 2 * most : 0;
+  size_t o = 0;
+  w.off = o;  o += up(sizeof(int32_t) * (D.n_adapters + 2));
+  w.perm = o; o += up(sizeof(int32_t) * static_cast<size_t>(n));
+  w.dv = o;   o += up(sizeof(float) * static_cast<size_t>(n) * D.rank);
+  for (int i = 0; i < 2; ++i) {
+    w.part[i] = o;
+    o += up(sizeof(float) * w.places * static_cast<size_t>(i ? D.in_dim : D.out_dim) * D.rank);
+  }
+  w.total = o;
+  return w;
+}
+
+template <typename T, int RT, int NT, bool BACK>
+cudaError_t launch_tile(const LowrankArgs& a, int tiles, int ctas, cudaStream_t st) {
+  using L = Lowrank<T, RT, NT, BACK>;
+  if (L::SMEM > 40 * 1024) {
+    const cudaError_t e = allow_smem<lowrank_kernel<T, RT, NT, BACK>>(static_cast<int>(L::SMEM));
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles) * ctas);
+  cfg.blockDim = dim3(LR_THREADS);
+  cfg.dynamicSmemBytes = L::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {static_cast<unsigned>(ctas), 1, 1};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = g_pdl_enabled ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, lowrank_kernel<T, RT, NT, BACK>, a);
+}
+
+template <typename T, bool BACK>
+cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
+  // Rows per tile by the mean rows of an adapter; CTAs per tile until the tiles fill the GPU twice.
+  const int groups = a.n < a.G ? a.n : a.G, mean = (a.n + groups - 1) / groups;
+  const int nt = mean <= 8 ? 1 : mean <= 48 || (sizeof(T) == 4 && a.rank > 32) ? 4 : 8;
+  const int full = (a.n + nt * 8 - 1) / (nt * 8), tiles = a.ids ? a.n : full + (a.segments < a.n ? a.segments : a.n);
+  const int busy = full > groups ? full : groups;
+  int ctas = 1;
+  while (ctas < 8 && busy * ctas * 2 <= 2 * GPU_SMS) ctas *= 2;
+  const auto by_rows = [&](auto rt) -> cudaError_t {
+    constexpr int RT = decltype(rt)::value;
+    if (nt == 1) return launch_tile<T, RT, 1, BACK>(a, tiles, ctas, st);
+    if (nt == 4) return launch_tile<T, RT, 4, BACK>(a, tiles, ctas, st);
+    if constexpr (sizeof(T) == 2 || RT < 4) return launch_tile<T, RT, 8, BACK>(a, tiles, ctas, st);
+    return cudaErrorInvalidValue;  // not reached: nt is 4 there
+  };
+  if (a.rank <= 16) return by_rows(std::integral_constant<int, 1>());
+  if (a.rank <= 32) return by_rows(std::integral_constant<int, 2>());
+  return by_rows(std::integral_constant<int, 4>());
+}
+
+template <typename T>
+cudaError_t launch_grads(const GradArgs& a, int chunks, cudaStream_t st) {
+  const dim3 grid(chunks, a.blocks[0] + a.blocks[1]);
+  if (a.rank <= 16) return launch_chain(lowrank_grad_kernel<T, 1>, grid, dim3(LR_THREADS), 0, st, a);
+  if (a.rank <= 32) return launch_chain(lowrank_grad_kernel<T, 2>, grid, dim3(LR_THREADS), 0, st, a);
+  return launch_chain(lowrank_grad_kernel<T, 4>, grid, dim3(LR_THREADS), 0, st, a);
+}
+
+int check_lowrank(const emoe_lowrank_desc* D, int n, const int32_t* ids, const int32_t* off) {
+  if (!D || n <= 0 || D->in_dim <= 0 || D->out_dim <= 0 || D->rank <= 0) return EMOE_ERR_INVALID_ARG;
+  if (D->n_adapters < 1 || D->n_adapters > EMOE_MAX_EXPERTS) return EMOE_ERR_INVALID_ARG;
+  if ((ids == nullptr) == (off == nullptr)) return EMOE_ERR_INVALID_ARG;
+  if ((D->x_stride && D->x_stride < D->in_dim) || (D->y_stride && D->y_stride < D->out_dim)) return EMOE_ERR_INVALID_ARG;
+  if (!dtype_ok(D->dtype) || D->rank > EMOE_MAX_RANK) return EMOE_ERR_UNSUPPORTED;
+  if (D->in_dim % 8 != 0 || D->out_dim % 8 != 0 || D->in_dim > 0x7fffffff / 64 || D->out_dim > 0x7fffffff / 64) return EMOE_ERR_UNSUPPORTED;
+  if (n > 0x7fffffff / 16) return EMOE_ERR_UNSUPPORTED;
+  const int64_t vec = 16 / static_cast<int64_t>(dtype_size(D->dtype));
+  if (D->x_stride % vec != 0 || D->y_stride % vec != 0) return EMOE_ERR_ALIGNMENT;
+  if (!ptr_aligned(ids, 4) || !ptr_aligned(off, 4)) return EMOE_ERR_ALIGNMENT;
+  return EMOE_OK;
+}
+
+}  // namespace
+}  // namespace emoe
+
+using namespace emoe;
+
+#define EMOE_CALL(ctx, call)                                    \
+  do {                                                          \
+    const cudaError_t e__ = (call);                             \
+    if (e__ != cudaSuccess) return ctx_cuda_fail(ctx, e__);     \
+  } while (0)
+
+extern "C" {
+
+size_t emoe_lowrank_workspace_bytes(const emoe_lowrank_desc* desc, int n) {
+  int32_t given = 0;
+  if (check_lowrank(desc, n, &given, nullptr) != EMOE_OK) return 0;
+  return lowrank_layout(*desc, n).total;  // grows with n
+}
+
+int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const void* A, const void* B, const float* scales, const void* x, int n,
+                         const int32_t* ids, const int32_t* off, const void* base, void* y, float* out_v, void* stream) {
+  const int rc = check_lowrank(desc, n, ids, off);
+  if (rc != EMOE_OK) return rc;
+  if (!A || !B || !x || !y) return EMOE_ERR_INVALID_ARG;
+  if (!ptr_aligned(A, 16) || !ptr_aligned(B, 16) || !ptr_aligned(x, 16) || !ptr_aligned(base, 16) || !ptr_aligned(y, 16) ||
+      !ptr_aligned(scales, 4) || !ptr_aligned(out_v, 4))
+    return EMOE_ERR_ALIGNMENT;
+  if (!ctx) return EMOE_ERR_INVALID_ARG;
+  const CallScope scope(ctx);
+  EMOE_CALL(ctx, scope.error());
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  LowrankArgs a = {};
+  a.x = x;
+  a.base = base;
+  a.down = A;
+  a.up = B;
+  a.scales = scales;
+  a.y = y;
+  a.v = out_v;
+  a.check_word = ctx_check_word(ctx);
+  a.n = n;
+  a.G = a.segments = desc->n_adapters;
+  a.rank = desc->rank;
+  a.in_dim = desc->in_dim;
+  a.out_dim = desc->out_dim;
+  a.skip_none = base == y;
+  a.x_stride = static_cast<size_t>(desc->x_stride ? desc->x_stride : desc->in_dim);
+  a.y_stride = static_cast<size_t>(desc->y_stride ? desc->y_stride : desc->out_dim);
+  a.off = off;
+  if (ids && n <= LR_IDS_ROWS) {
+    a.ids = ids;
+  } else if (ids) {
+    size_t have = 0;
+    char* ws = ctx_workspace(ctx, &have);
+    const LowrankLayout w = lowrank_layout(*desc, n);
+    if (w.dv > have) return EMOE_ERR_WORKSPACE;  // the order is all that the forward pass keeps there
+    int32_t *off_ws = reinterpret_cast<int32_t*>(ws + w.off), *perm = reinterpret_cast<int32_t*>(ws + w.perm);
+    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, nullptr, a.check_word, st));
+    a.off = off_ws;
+    a.perm = perm;
+    a.segments = desc->n_adapters + 1;
+  }
+  EMOE_CALL(ctx, desc->dtype == EMOE_DTYPE_BF16 ? (launch_lowrank<__nv_bfloat16, false>(a, st)) : (launch_lowrank<float, false>(a, st)));
+  return EMOE_OK;
+}
+
+int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const void* A, const void* B, const float* scales, const void* x,
+                          const void* dy, int n, const int32_t* ids, const int32_t* off, const float* v, const void* dx_base, void* dx, float* dA,
+                          float* dB, void* stream) {
+  const int rc = check_lowrank(desc, n, ids, off);
+  if (rc != EMOE_OK) return rc;
+  if (!dy || (!dx && !dA && !dB)) return EMOE_ERR_INVALID_ARG;
+  if (((dx || dA) && !B) || (dx && !A) || (dA && !x) || (dB && !v)) return EMOE_ERR_INVALID_ARG;
+  if (!ptr_aligned(A, 16) || !ptr_aligned(B, 16) || !ptr_aligned(x, 16) || !ptr_aligned(dy, 16) || !ptr_aligned(dx_base, 16) || !ptr_aligned(dx, 16) ||
+      !ptr_aligned(dA, 16) || !ptr_aligned(dB, 16) || !ptr_aligned(scales, 4) || !ptr_aligned(v, 4))
+    return EMOE_ERR_ALIGNMENT;
+  if (!ctx) return EMOE_ERR_INVALID_ARG;
+  size_t have = 0;
+  char* ws = ctx_workspace(ctx, &have);
+  const LowrankLayout w = lowrank_layout(*desc, n);
+  if (w.total > have) return EMOE_ERR_WORKSPACE;
+  const CallScope scope(ctx);
+  EMOE_CALL(ctx, scope.error());
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int32_t *off_ws = reinterpret_cast<int32_t*>(ws + w.off), *perm = reinterpret_cast<int32_t*>(ws + w.perm);
+  float* dv = reinterpret_cast<float*>(ws + w.dv);
+  LowrankArgs a = {};
+  a.x = dy;
+  a.base = dx_base;
+  a.down = B;
+  a.up = A;
+  a.scales = scales;
+  a.y = dx;
+  a.v = dA ? dv : nullptr;
+  a.check_word = ctx_check_word(ctx);
+  a.n = n;
+  a.G = a.segments = desc->n_adapters;
+  a.rank = desc->rank;
+  a.in_dim = desc->out_dim;
+  a.out_dim = desc->in_dim;
+  a.skip_none = dx_base == dx;
+  a.x_stride = static_cast<size_t>(desc->y_stride ? desc->y_stride : desc->out_dim);
+  a.y_stride = static_cast<size_t>(desc->x_stride ? desc->x_stride : desc->in_dim);
+  a.off = off;
+  if (ids) {
+    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, nullptr, a.check_word, st));
+    a.off = off_ws;
+    a.perm = perm;
+    a.segments = desc->n_adapters + 1;
+  }
+  const bool bf16 = desc->dtype == EMOE_DTYPE_BF16;
+  if (dx || dA) EMOE_CALL(ctx, bf16 ? (launch_lowrank<__nv_bfloat16, true>(a, st)) : (launch_lowrank<float, true>(a, st)));
+  if (!dA && !dB) return EMOE_OK;
+  GradArgs ga = {};
+  ga.act[0] = dy;
+  ga.act[1] = x;
+  ga.vec[0] = v;
+  ga.vec[1] = dv;
+  ga.stride[0] = a.x_stride;
+  ga.stride[1] = a.y_stride;
+  ga.dim[0] = desc->out_dim;
+  ga.dim[1] = desc->in_dim;
+  ga.out[0] = dB;
+  ga.out[1] = dA;
+  ga.scales = scales;
+  ga.off = a.off;
+  ga.perm = a.perm;
+  ga.check_word = a.check_word;
+  ga.places = w.places;
+  ga.n = n;
+  ga.G = desc->n_adapters;
+  ga.rank = desc->rank;
+  ga.chunk_rows = w.chunk_rows;
+  for (int i = 0; i < 2; ++i) {
+    ga.part[i] = reinterpret_cast<float*>(ws + w.part[i]);
+    ga.blocks[i] = ga.out[i] ? (ga.dim[i] + GR_CHANNELS - 1) / GR_CHANNELS : 0;
+  }
+  const int chunks = w.chunks + (ga.G < n ? ga.G : n);
+  EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, chunks, st) : launch_grads<float>(ga, chunks, st));
+  EMOE_CALL(ctx, launch_chain(lowrank_join_kernel, dim3(ga.G, 8), dim3(LR_THREADS), 0, st, ga));
+  return EMOE_OK;
+}
+
+}  // extern "C"

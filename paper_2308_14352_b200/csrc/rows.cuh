@@ -111,8 +111,9 @@ inline size_t dtype_size(int dtype) { return dtype == EMOE_DTYPE_F32 ? 4 : 2; }
 inline bool ptr_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // Stable counting sort of n ids by one cluster of CTAs (dispatch.cu): the outputs of emoe_permute.  counts and slot_of_pair may be null.
-// bad_flag: whether an id outside [0, E) other than `none` sets the check word.
-cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, int none, int32_t* counts, int32_t* off, int32_t* perm, int32_t* slot_of_pair,
+// rest: ids outside [0, E - 1) are sorted into the last of the E lists, and only those other than -1 set the check word; else ids
+// outside [0, E) are dropped and set it.
+cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32_t* counts, int32_t* off, int32_t* perm, int32_t* slot_of_pair,
                               int* check_word, cudaStream_t st);
 
 }  // namespace emoe
