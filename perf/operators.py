@@ -249,7 +249,7 @@ def _library():
     if not _handle:
         from paper_2308_14352_b200 import binding as B
 
-        most = B.emoe_lowrank_desc(64, 64, 14336, 14336, B.DTYPE_F32, 0, 0, 0)
+        most = B.emoe_lowrank_desc(64, 64, 14336, 14336, B.DTYPE_BF16, 0, 0, 0)
         _handle.update(B=B, ctx=B.emoe_create(torch.cuda.current_device(), B.emoe_lowrank_workspace_bytes(most, 16384)),
                        dtype={torch.float32: B.DTYPE_F32, torch.bfloat16: B.DTYPE_BF16})
     return _handle
