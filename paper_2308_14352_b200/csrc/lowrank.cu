@@ -15,62 +15,14 @@
 // (2^-24 of the product) are left out.
 #include <cooperative_groups.h>
 
-#include "rows.cuh"
+#include "lowrank.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace emoe {
 namespace {
 
-constexpr int LR_THREADS = 256, LR_WARPS = LR_THREADS / 32;
 constexpr int LR_IDS_ROWS = 512;  // most rows whose adapters every CTA looks up by itself
-
-__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// Two fp32 values as N pairs of bf16 parts, largest first.  All parts but the last are truncated: what is left is exact, so three
-// parts are the value itself.  An infinity has no rest.
-template <int N>
-__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
-    if (N == 2 && i == N - 1) {
-      const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
-      part[i] = *reinterpret_cast<const uint32_t*>(&r);
-    } else {
-      part[i] = __byte_perm(ua, ub, 0x7632);
-    }
-    a = isinf(a) ? 0.f : a - __uint_as_float(ua & 0xffff0000u);
-    b = isinf(b) ? 0.f : b - __uint_as_float(ub & 0xffff0000u);
-  }
-}
-
-template <typename T>
-struct Parts {  // bf16 parts of a factor or activation, and of the fp32 vector it is multiplied with
-  static constexpr int IN = sizeof(T) == 4 ? 3 : 1;
-  static constexpr int VEC = sizeof(T) == 4 ? 3 : 2;
-};
-
-// a . b over the kept products of their parts
-template <int PA, int PB>
-__device__ __forceinline__ void mma_parts(float (&d)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][2]) {
-#pragma unroll
-  for (int i = PA - 1; i >= 0; --i)  // smallest first
-#pragma unroll
-    for (int j = PB - 1; j >= 0; --j)
-      if (i + j < 3) mma_bf16(d, a[i], b[j][0], b[j][1]);
-}
-
-__device__ __forceinline__ uint4 load16(const void* p) {
-  uint32_t w[4];
-  load_words(p, w);
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ uint4 load16_keep(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
 struct LowrankArgs {
   const void *x, *base;  // rows in, rows added to the result (null: zeros)
@@ -526,70 +478,24 @@ struct GradArgs {
   const int32_t *off, *perm;
   float* part[2];         // [chunks of adapters with several][dim][rank]
   int* check_word;
-  int n, G, rank, chunk_rows, blocks[2], places;
+  int n, G, rank, chunk_rows[2], blocks[2], places[2];
 };
-
-// Chunk `c` of the list of all adapters' chunks: adapter, first row and rows, number of its adapter's chunks and its place among the chunks of
-// adapters with several; false: no such chunk.  Every thread calls it.
-struct Chunk {
-  int adapter, begin, rows, of_adapter, place;
-};
-__device__ __forceinline__ bool find_chunk(const GradArgs& a, int c, int* s_scan, Chunk* out) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int begin = 0, rows = 0;
-  if (tid < a.G) {
-    begin = min(max(a.off[tid], 0), a.n);
-    rows = max(min(a.off[tid + 1], a.n) - begin, 0);
-  }
-  const int chunks = (rows + a.chunk_rows - 1) / a.chunk_rows, several = chunks > 1 ? chunks : 0;
-  int i0 = chunks, i1 = several;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u0 = __shfl_up_sync(0xffffffffu, i0, o), u1 = __shfl_up_sync(0xffffffffu, i1, o);
-    if (lane >= o) {
-      i0 += u0;
-      i1 += u1;
-    }
-  }
-  if (lane == 31) {
-    s_scan[warp] = i0;
-    s_scan[LR_WARPS + warp] = i1;
-  }
-  if (tid == 0) s_scan[2 * LR_WARPS] = -1;
-  __syncthreads();
-  int f0 = i0 - chunks, f1 = i1 - several;
-  for (int w = 0; w < warp; ++w) {
-    f0 += s_scan[w];
-    f1 += s_scan[LR_WARPS + w];
-  }
-  if (c >= f0 && c < f0 + chunks) {
-    s_scan[2 * LR_WARPS] = tid;
-    s_scan[2 * LR_WARPS + 1] = begin + (c - f0) * a.chunk_rows;
-    s_scan[2 * LR_WARPS + 2] = min(a.chunk_rows, rows - (c - f0) * a.chunk_rows);
-    s_scan[2 * LR_WARPS + 3] = chunks;
-    s_scan[2 * LR_WARPS + 4] = f1 + (c - f0);
-  }
-  __syncthreads();
-  const int* s = s_scan + 2 * LR_WARPS;
-  *out = {s[0], s[1], s[2], s[3], s[4]};
-  return s[0] >= 0;
-}
 
 template <typename T, int RT>
 __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a) {
   constexpr int NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
   __shared__ uint32_t s_vec[3][PAIRS][W_STRIDE];
-  __shared__ int s_rows[GR_ROWS], s_scan[2 * LR_WARPS + 5];
+  __shared__ int s_rows[GR_ROWS], s_scan[CHUNK_SCAN];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
   pdl_wait();
   pdl_trigger();
+  const int which = static_cast<int>(blockIdx.y) >= a.blocks[0], block = blockIdx.y - (which ? a.blocks[0] : 0);
   Chunk ch;
-  if (!find_chunk(a, blockIdx.x, s_scan, &ch)) return;
-  if (ch.of_adapter > 1 && ch.place >= a.places) {  // only where the segments overlap
+  if (!find_chunk(a.off, a.G, a.G, a.n, a.chunk_rows[which], blockIdx.x, s_scan, &ch)) return;
+  if (ch.of_adapter > 1 && ch.place >= a.places[which]) {  // only where the segments overlap
     if (tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
     return;
   }
-  const int which = static_cast<int>(blockIdx.y) >= a.blocks[0], block = blockIdx.y - (which ? a.blocks[0] : 0);
   const int dim = a.dim[which], c0 = block * GR_CHANNELS + warp * 64 + 8 * g;  // this lane's eight channels
   const T* act = static_cast<const T*>(a.act[which]);
   const float* vec = a.vec[which];
@@ -649,7 +555,13 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
 #pragma unroll
           for (int half = 0; half < 2; ++half) bf[j][half] = s_vec[j][k / 2 + 2 * q + half][nr * 8 + g];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) mma_parts<PI, 3>(acc[m][nr], af[m], bf);
+        for (int m = 0; m < 4; ++m) {
+          // the tensor cores cut what they add: sixteen rows are summed by themselves, then added with rounding
+          float d[4] = {};
+          mma_parts<PI, 3>(d, af[m], bf);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[m][nr][i] += d[i];
+        }
       }
     }
   }
@@ -674,16 +586,18 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
     }
 }
 
-// Joins the chunks of adapters with several, in order, and clears the gradients of adapters without rows.
+// Joins the chunks of adapters with several, in order, and clears the gradients of adapters without rows.  grid: (adapters, shares of a
+// gradient, dB and dA)
 __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
-  __shared__ int s_scan[2 * LR_WARPS];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, adapter = blockIdx.x;
+  __shared__ int s_scan[LR_WARPS + 1];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, adapter = blockIdx.x, which = blockIdx.z;
   pdl_wait();
   pdl_trigger();
+  if (!a.out[which]) return;
   int several = 0, chunks = 0;
   if (tid < a.G) {
-    const int rows = max(min(a.off[tid + 1], a.n) - min(max(a.off[tid], 0), a.n), 0);
-    chunks = (rows + a.chunk_rows - 1) / a.chunk_rows;
+    const int begin = min(max(a.off[tid], 0), a.n), rows = max(min(a.off[tid + 1], a.n) - begin, 0);
+    chunks = (rows + a.chunk_rows[which] - 1) / a.chunk_rows[which];
     several = chunks > 1 ? chunks : 0;
   }
   const int front = __reduce_add_sync(0xffffffffu, tid < adapter ? several : 0);
@@ -694,48 +608,61 @@ __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
   if (mine == 1) return;
   int place = 0;
   for (int w = 0; w < LR_WARPS; ++w) place += s_scan[w];
-  if (place + mine > a.places && mine > 1) return;
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    if (!a.out[which]) continue;
-    const size_t size = static_cast<size_t>(a.dim[which]) * a.rank;  // dim is a multiple of 8
-    float4* out = reinterpret_cast<float4*>(a.out[which] + adapter * size);
-    const float4* in = reinterpret_cast<const float4*>(a.part[which] + place * size);
-    for (size_t i = static_cast<size_t>(blockIdx.y) * LR_THREADS + tid; i < size / 4; i += static_cast<size_t>(gridDim.y) * LR_THREADS) {
-      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int c = 0; c < mine; ++c) {
-        const float4 u = in[c * (size / 4) + i];
-        s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
-      }
-      out[i] = s;
+  if (mine > 1 && place + mine > a.places[which]) return;
+  const size_t words = static_cast<size_t>(a.dim[which]) * a.rank / 4;  // dim is a multiple of 8
+  float4* out = reinterpret_cast<float4*>(a.out[which]) + adapter * words;
+  const float4* in = reinterpret_cast<const float4*>(a.part[which]) + place * words;
+  for (size_t i = static_cast<size_t>(blockIdx.y) * LR_THREADS + tid; i < words; i += static_cast<size_t>(gridDim.y) * LR_THREADS) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int c = 0; c < mine; ++c) {
+      const float4 u = in[c * words + i];
+      s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
     }
+    out[i] = s;
   }
 }
 
 // ---- launches -----------------------------------------------------------------------------------
 
+// Rows from which bf16 calls take the streaming kernels.
+constexpr int LR_STREAM_ROWS = 512;
+
 struct LowrankLayout {
-  size_t off, perm, dv, part[2], total;
-  int chunk_rows, chunks, places;
+  size_t off, perm, vec, planes, part[2], total;  // vec: dv, or the vectors in the order; planes: their shares
+  int chunk_rows[2], chunks[2], places[2];        // of the gradients: dB, dA
 };
+
+// Chunks of rows so that `blocks` CTAs each make about `ctas` in all: whole rows of tiles, no more than a CTA lists.
+int chunk_rows_for(int n, int blocks, int ctas) {
+  const int wanted = (ctas + blocks - 1) / blocks, rows = ((n + wanted - 1) / wanted + 63) / 64 * 64;
+  return rows < 2048 ? rows : 2048;
+}
+int blocks_of(int dim) { return (dim + ST_CHANNELS - 1) / ST_CHANNELS; }
+bool takes_stream(const emoe_lowrank_desc& D, int n) { return D.dtype == EMOE_DTYPE_BF16 && n > LR_STREAM_ROWS; }
 
 LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
   const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   LowrankLayout w{};
-  // chunks of rows for the factors' gradients: some two CTAs per SM over both products, at least 64 rows each
-  const int blocks = (D.in_dim + GR_CHANNELS - 1) / GR_CHANNELS + (D.out_dim + GR_CHANNELS - 1) / GR_CHANNELS;
-  const int wanted = (2 * GPU_SMS + blocks - 1) / blocks, most = wanted < (n + GR_ROWS - 1) / GR_ROWS ? wanted : (n + GR_ROWS - 1) / GR_ROWS;
-  w.chunk_rows = ((n + wanted - 1) / wanted + GR_ROWS - 1) / GR_ROWS * GR_ROWS;
-  w.chunks = (n + w.chunk_rows - 1) / w.chunk_rows;  // at most `most`, which grows with n
-  // An adapter with several chunks fills all of them but one, so that there are no more than twice as many of those as all rows together make.
-  w.places = most > 1 ? 2 * most : 0;
+  const size_t vectors = sizeof(float) * static_cast<size_t>(n) * D.rank;
   size_t o = 0;
   w.off = o;  o += up(sizeof(int32_t) * (D.n_adapters + 2));
   w.perm = o; o += up(sizeof(int32_t) * static_cast<size_t>(n));
-  w.dv = o;   o += up(sizeof(float) * static_cast<size_t>(n) * D.rank);
+  w.vec = o;  o += up(vectors);
+  w.planes = o;
+  if (takes_stream(D, n)) o += up(vectors * blocks_of(D.in_dim > D.out_dim ? D.in_dim : D.out_dim));
   for (int i = 0; i < 2; ++i) {
+    const int dim = i ? D.in_dim : D.out_dim, blocks = blocks_of(dim);
+    w.chunk_rows[i] = chunk_rows_for(n, blocks, 2 * GPU_SMS);
+    w.chunks[i] = (n + w.chunk_rows[i] - 1) / w.chunk_rows[i];
+    // An adapter with several chunks fills all of them but one, so that there are no more than twice as many of those as all rows together
+    // make.  The room for them grows with n, dim and rank alike (wanted * dim <= ctas * ST_CHANNELS + dim): a context that is made for the
+    // largest call serves all.
+    const size_t tiles = (n + 63) / 64, lists = (n + 2047) / 2048, even = static_cast<size_t>(2 * GPU_SMS) * ST_CHANNELS + dim;
+    const size_t values = (tiles * dim < even ? tiles * dim : even > lists * dim ? even : lists * dim) * 2;
+    w.places[i] = static_cast<int>(values / dim < 0x7fffffff ? values / dim : 0x7fffffff);
     w.part[i] = o;
-    o += up(sizeof(float) * w.places * static_cast<size_t>(i ? D.in_dim : D.out_dim) * D.rank);
+    o += up(sizeof(float) * values * D.rank);
   }
   w.total = o;
   return w;
@@ -784,12 +711,85 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
   return by_rows(std::integral_constant<int, 4>());
 }
 
+cudaError_t launch_join(const GradArgs& a, cudaStream_t st) {
+  const size_t dim = a.dim[0] > a.dim[1] ? a.dim[0] : a.dim[1], shares = (dim * a.rank / 4 + LR_THREADS - 1) / LR_THREADS;
+  return launch_chain(lowrank_join_kernel, dim3(a.G, static_cast<unsigned>(shares < 32 ? shares : 32), 2), dim3(LR_THREADS), 0, st, a);
+}
+
 template <typename T>
 cudaError_t launch_grads(const GradArgs& a, int chunks, cudaStream_t st) {
   const dim3 grid(chunks, a.blocks[0] + a.blocks[1]);
   if (a.rank <= 16) return launch_chain(lowrank_grad_kernel<T, 1>, grid, dim3(LR_THREADS), 0, st, a);
   if (a.rank <= 32) return launch_chain(lowrank_grad_kernel<T, 2>, grid, dim3(LR_THREADS), 0, st, a);
   return launch_chain(lowrank_grad_kernel<T, 4>, grid, dim3(LR_THREADS), 0, st, a);
+}
+
+// Many bf16 rows: rows that go down and, backward, the outer products; the vectors' sum; rows that come up.
+cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, char* ws, const LowrankLayout& w, cudaStream_t st) {
+  using bf16 = __nv_bfloat16;
+  const int segments = a.G < a.n ? a.G : a.n;
+  float *vec = reinterpret_cast<float*>(ws + w.vec), *planes = reinterpret_cast<float*>(ws + w.planes);
+  const bool vectors = a.y || a.v || (back && ga->out[1]);
+  const auto outer = [&](int which, StreamArgs* s) {
+    s->vec = which ? vec : ga->vec[0];
+    s->vec_by_place = which;
+    s->scales = a.scales;
+    s->out = ga->out[which];
+    s->part = ga->part[which];
+    s->rank_major = which;
+    s->chunk_rows = w.chunk_rows[which];
+    s->places = w.places[which];
+  };
+  StreamArgs s = {};
+  s.act = static_cast<const bf16*>(a.x);
+  s.stride = a.x_stride;
+  s.dim = a.in_dim;
+  s.factor = vectors ? static_cast<const bf16*>(a.down) : nullptr;
+  s.by_channel = back;
+  s.planes = planes;
+  s.off = a.off;
+  s.perm = a.perm;
+  s.check_word = a.check_word;
+  s.n = a.n;
+  s.G = a.G;
+  s.rank = a.rank;
+  s.chunk_rows = chunk_rows_for(a.n, blocks_of(a.in_dim), 3 * GPU_SMS);
+  if (back && ga->out[0]) outer(0, &s);
+  cudaError_t e = cudaSuccess;
+  if (s.factor || s.vec) e = launch_lowrank_stream(s, (a.n + s.chunk_rows - 1) / s.chunk_rows + segments, st);
+  if (e != cudaSuccess || !vectors) return e;
+  SumArgs u = {planes, blocks_of(a.in_dim), vec, a.v, a.off, a.perm, a.n, a.G, a.rank, a.segments > a.G};
+  e = launch_lowrank_sum(u, st);
+  if (e != cudaSuccess) return e;
+  if (a.y) {
+    UpArgs p = {};
+    p.vec = vec;
+    p.scales = a.scales;
+    p.factor = static_cast<const bf16*>(a.up);
+    p.by_rank = back;
+    p.base = static_cast<const bf16*>(a.base);
+    p.out = static_cast<bf16*>(a.y);
+    p.stride = a.y_stride;
+    p.dim = a.out_dim;
+    p.off = a.off;
+    p.perm = a.perm;
+    p.n = a.n;
+    p.G = a.G;
+    p.segments = a.segments;
+    p.rank = a.rank;
+    p.chunk_rows = chunk_rows_for(a.n, blocks_of(a.out_dim), 4 * GPU_SMS);
+    p.skip_none = a.skip_none;
+    e = launch_lowrank_up(p, (a.n + p.chunk_rows - 1) / p.chunk_rows + (a.segments < a.n ? a.segments : a.n), st);
+    if (e != cudaSuccess) return e;
+  }
+  if (!back || !ga->out[1]) return cudaSuccess;
+  StreamArgs x = s;
+  x.act = static_cast<const bf16*>(ga->act[1]);
+  x.stride = ga->stride[1];
+  x.dim = ga->dim[1];
+  x.factor = nullptr;
+  outer(1, &x);
+  return launch_lowrank_stream(x, w.chunks[1] + segments, st);
 }
 
 int check_lowrank(const emoe_lowrank_desc* D, int n, const int32_t* ids, const int32_t* off) {
@@ -855,20 +855,23 @@ int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const voi
   a.x_stride = static_cast<size_t>(desc->x_stride ? desc->x_stride : desc->in_dim);
   a.y_stride = static_cast<size_t>(desc->y_stride ? desc->y_stride : desc->out_dim);
   a.off = off;
+  size_t have = 0;
+  char* ws = ctx_workspace(ctx, &have);
+  const LowrankLayout w = lowrank_layout(*desc, n);
   if (ids && n <= LR_IDS_ROWS) {
     a.ids = ids;
+  } else if (off && takes_stream(*desc, n)) {
+    if (w.part[0] > have) return EMOE_ERR_WORKSPACE;
   } else if (ids) {
-    size_t have = 0;
-    char* ws = ctx_workspace(ctx, &have);
-    const LowrankLayout w = lowrank_layout(*desc, n);
-    if (w.dv > have) return EMOE_ERR_WORKSPACE;  // the order is all that the forward pass keeps there
+    if ((takes_stream(*desc, n) ? w.part[0] : w.vec) > have) return EMOE_ERR_WORKSPACE;
     int32_t *off_ws = reinterpret_cast<int32_t*>(ws + w.off), *perm = reinterpret_cast<int32_t*>(ws + w.perm);
     EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, nullptr, a.check_word, st));
     a.off = off_ws;
     a.perm = perm;
     a.segments = desc->n_adapters + 1;
   }
-  EMOE_CALL(ctx, desc->dtype == EMOE_DTYPE_BF16 ? (launch_lowrank<__nv_bfloat16, false>(a, st)) : (launch_lowrank<float, false>(a, st)));
+  if (takes_stream(*desc, n)) EMOE_CALL(ctx, launch_many(a, false, nullptr, ws, w, st));
+  else EMOE_CALL(ctx, desc->dtype == EMOE_DTYPE_BF16 ? (launch_lowrank<__nv_bfloat16, false>(a, st)) : (launch_lowrank<float, false>(a, st)));
   return EMOE_OK;
 }
 
@@ -891,7 +894,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   EMOE_CALL(ctx, scope.error());
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int32_t *off_ws = reinterpret_cast<int32_t*>(ws + w.off), *perm = reinterpret_cast<int32_t*>(ws + w.perm);
-  float* dv = reinterpret_cast<float*>(ws + w.dv);
+  float* dv = reinterpret_cast<float*>(ws + w.vec);
   LowrankArgs a = {};
   a.x = dy;
   a.base = dx_base;
@@ -899,7 +902,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   a.up = A;
   a.scales = scales;
   a.y = dx;
-  a.v = dA ? dv : nullptr;
+  a.v = dA && !takes_stream(*desc, n) ? dv : nullptr;
   a.check_word = ctx_check_word(ctx);
   a.n = n;
   a.G = a.segments = desc->n_adapters;
@@ -916,9 +919,6 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
     a.perm = perm;
     a.segments = desc->n_adapters + 1;
   }
-  const bool bf16 = desc->dtype == EMOE_DTYPE_BF16;
-  if (dx || dA) EMOE_CALL(ctx, bf16 ? (launch_lowrank<__nv_bfloat16, true>(a, st)) : (launch_lowrank<float, true>(a, st)));
-  if (!dA && !dB) return EMOE_OK;
   GradArgs ga = {};
   ga.act[0] = dy;
   ga.act[1] = x;
@@ -934,18 +934,25 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   ga.off = a.off;
   ga.perm = a.perm;
   ga.check_word = a.check_word;
-  ga.places = w.places;
   ga.n = n;
   ga.G = desc->n_adapters;
   ga.rank = desc->rank;
-  ga.chunk_rows = w.chunk_rows;
   for (int i = 0; i < 2; ++i) {
     ga.part[i] = reinterpret_cast<float*>(ws + w.part[i]);
     ga.blocks[i] = ga.out[i] ? (ga.dim[i] + GR_CHANNELS - 1) / GR_CHANNELS : 0;
+    ga.chunk_rows[i] = w.chunk_rows[i];
+    ga.places[i] = w.places[i];
   }
-  const int chunks = w.chunks + (ga.G < n ? ga.G : n);
-  EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, chunks, st) : launch_grads<float>(ga, chunks, st));
-  EMOE_CALL(ctx, launch_chain(lowrank_join_kernel, dim3(ga.G, 8), dim3(LR_THREADS), 0, st, ga));
+  const int none_or_one = ga.G < n ? ga.G : n;  // segments that do not end on a chunk's end
+  if (takes_stream(*desc, n)) {
+    EMOE_CALL(ctx, launch_many(a, true, &ga, ws, w, st));
+  } else {
+    const bool bf16 = desc->dtype == EMOE_DTYPE_BF16;
+    if (dx || dA) EMOE_CALL(ctx, bf16 ? (launch_lowrank<__nv_bfloat16, true>(a, st)) : (launch_lowrank<float, true>(a, st)));
+    const int chunks = (w.chunks[0] > w.chunks[1] ? w.chunks[0] : w.chunks[1]) + none_or_one;
+    if (dA || dB) EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, chunks, st) : launch_grads<float>(ga, chunks, st));
+  }
+  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, st));
   return EMOE_OK;
 }
 
