@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) gather_kernel(RowsArgs a) {
 // (match gives the lanes of an expert and their ranks), the counts of all warps in front of it, of its CTA and of the CTAs before (read
 // over distributed shared memory), are its first places, and a second walk hands them out.  Two cluster-wide waits,
 // no order-dependent atomics.  keep_rest: ids outside [0, E - 1) count as E - 1.
-constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CLUSTER = 8;
+constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CLUSTER = 8, SORT_STEPS = 8;
 
 __global__ void __launch_bounds__(SORT_THREADS)
     sort_pairs_kernel(const int32_t* __restrict__ ids, int n, int E, bool keep_rest, int32_t* __restrict__ counts, int32_t* __restrict__ off,
@@ -204,17 +204,28 @@ __global__ void __launch_bounds__(SORT_THREADS)
   pdl_wait();
   pdl_trigger();
   bool bad = false;
-  for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32) {
-    const int p = p0 + lane;
-    int id = p < n ? ids[p] : -1;
-    if (p < n && (id < 0 || id >= named)) {
-      bad |= !keep_rest || id != -1;
-      id = rest;
+  int id[SORT_STEPS];  // ids of eight steps are asked for together; a run of no more is read once
+  const auto load = [&](int p0) {
+#pragma unroll
+    for (int i = 0; i < SORT_STEPS; ++i) {
+      const int p = p0 + 32 * i + lane;
+      const bool live = 32 * i < run - (p0 - begin) && p < n;
+      id[i] = live ? ids[p] : -1;
+      if (live && (id[i] < 0 || id[i] >= named)) {
+        bad |= !keep_rest || id[i] != -1;
+        id[i] = rest;
+      }
     }
-    const bool ok = id >= 0;
-    const unsigned same = __match_any_sync(0xffffffffu, id);
-    if (ok && lane == __ffs(same) - 1) mine[id] += __popc(same);
-    __syncwarp();
+  };
+  for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32 * SORT_STEPS) {
+    load(p0);
+#pragma unroll
+    for (int i = 0; i < SORT_STEPS; ++i) {
+      if (p0 + 32 * i >= begin + run || p0 + 32 * i >= n) break;
+      const unsigned same = __match_any_sync(0xffffffffu, id[i]);
+      if (id[i] >= 0 && lane == __ffs(same) - 1) mine[id[i]] += __popc(same);
+      __syncwarp();
+    }
   }
   if (bad) atomicOr(check_word, CHECK_BAD_EXPERT_ID);
   __syncthreads();
@@ -264,21 +275,23 @@ __global__ void __launch_bounds__(SORT_THREADS)
   // pairs without an expert own no place: what lies behind the last one reads as "no pair"
   for (int p = s_off[E] + rank * SORT_THREADS + tid; p < n; p += ctas * SORT_THREADS) perm[p] = -1;
   __syncthreads();
-  for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32) {
-    const int p = p0 + lane;
-    int id = p < n ? ids[p] : -1;
-    if (id >= named || id < 0) id = p < n ? rest : -1;
-    const bool ok = id >= 0;
-    const unsigned same = __match_any_sync(0xffffffffu, id);
-    int pos = -1;
-    if (ok) {
-      pos = mine[id] + __popc(same & ((1u << lane) - 1u));
-      perm[pos] = p;
+  for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32 * SORT_STEPS) {
+    if (run > 32 * SORT_STEPS) load(p0);
+#pragma unroll
+    for (int i = 0; i < SORT_STEPS; ++i) {
+      if (p0 + 32 * i >= begin + run || p0 + 32 * i >= n) break;
+      const int p = p0 + 32 * i + lane, e = id[i];
+      const unsigned same = __match_any_sync(0xffffffffu, e);
+      int pos = -1;
+      if (e >= 0) {
+        pos = mine[e] + __popc(same & ((1u << lane) - 1u));
+        perm[pos] = p;
+      }
+      if (p < n && slot_of_pair) slot_of_pair[p] = pos;
+      __syncwarp();
+      if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+      __syncwarp();
     }
-    if (p < n && slot_of_pair) slot_of_pair[p] = pos;
-    __syncwarp();
-    if (ok && lane == __ffs(same) - 1) mine[id] += __popc(same);
-    __syncwarp();
   }
   cluster.sync();  // nobody leaves while another CTA reads its counts
 }

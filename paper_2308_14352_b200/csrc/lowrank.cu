@@ -633,32 +633,40 @@ struct LowrankLayout {
   int chunk_rows[2], chunks[2], places[2];        // of the gradients: dB, dA
 };
 
-// Chunks of rows so that `blocks` CTAs each make about `ctas` in all: whole rows of tiles, no more than a CTA lists.
-int chunk_rows_for(int n, int blocks, int ctas) {
-  const int wanted = (ctas + blocks - 1) / blocks, rows = ((n + wanted - 1) / wanted + 63) / 64 * 64;
-  return rows < 2048 ? rows : 2048;
+// Rows per chunk of the kernels on many rows, for `blocks` CTAs per chunk where the GPU holds `slots` at once: the fewest rows with which
+// all CTAs run side by side (a few left over would take as long again), a segment's last chunk counted as whole.  Many segments
+// make several rounds of CTAs whatever the chunks: then twice the mean segment, so that a long one is shared out.
+int chunk_rows_for(int n, int segments, int blocks, int slots, int tile, int most) {
+  const int chunks = slots / blocks - segments, mean = (n + segments - 1) / segments;
+  int rows = chunks > 0 ? (n + chunks - 1) / chunks : 2 * mean > 256 ? 2 * mean : 256;
+  if (rows > most) rows = most;
+  return (rows + tile - 1) / tile * tile;
 }
-int blocks_of(int dim) { return (dim + ST_CHANNELS - 1) / ST_CHANNELS; }
+int blocks_of(int dim, int channels) { return (dim + channels - 1) / channels; }
 bool takes_stream(const emoe_lowrank_desc& D, int n) { return D.dtype == EMOE_DTYPE_BF16 && n > LR_STREAM_ROWS; }
 
 LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
   const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   LowrankLayout w{};
+  const int segments = D.n_adapters < n ? D.n_adapters : n;
   const size_t vectors = sizeof(float) * static_cast<size_t>(n) * D.rank;
   size_t o = 0;
   w.off = o;  o += up(sizeof(int32_t) * (D.n_adapters + 2));
   w.perm = o; o += up(sizeof(int32_t) * static_cast<size_t>(n));
   w.vec = o;  o += up(vectors);
   w.planes = o;
-  if (takes_stream(D, n)) o += up(vectors * blocks_of(D.in_dim > D.out_dim ? D.in_dim : D.out_dim));
+  const bool stream = takes_stream(D, n);
+  const int channels = stream ? stream_channels(D.rank) : GR_CHANNELS;
+  if (stream) o += up(vectors * blocks_of(D.in_dim > D.out_dim ? D.in_dim : D.out_dim, channels));
   for (int i = 0; i < 2; ++i) {
-    const int dim = i ? D.in_dim : D.out_dim, blocks = blocks_of(dim);
-    w.chunk_rows[i] = chunk_rows_for(n, blocks, 2 * GPU_SMS);
+    const int dim = i ? D.in_dim : D.out_dim, blocks = blocks_of(dim, channels);
+    w.chunk_rows[i] = chunk_rows_for(n, segments, blocks, GPU_SMS, stream ? STREAM_ROWS : GR_ROWS, STREAM_MOST);
     w.chunks[i] = (n + w.chunk_rows[i] - 1) / w.chunk_rows[i];
     // An adapter with several chunks fills all of them but one, so that there are no more than twice as many of those as all rows together
-    // make.  The room for them grows with n, dim and rank alike (wanted * dim <= ctas * ST_CHANNELS + dim): a context that is made for the
-    // largest call serves all.
-    const size_t tiles = (n + 63) / 64, lists = (n + 2047) / 2048, even = static_cast<size_t>(2 * GPU_SMS) * ST_CHANNELS + dim;
+    // make: n over the rows of a chunk, which are slots / blocks of all or more, 1024 at most, or twice the mean segment.  The room for them
+    // grows with n, dim and rank alike (slots / blocks * dim <= slots * channels), so that a context that is made for the largest call serves all.
+    const size_t tiles = (n + 63) / 64, lists = (n + STREAM_MOST - 1) / STREAM_MOST, by_mean = (segments + 1) / 2 + 1;
+    const size_t even = static_cast<size_t>(GPU_SMS) * 512 + (by_mean + 1) * dim;
     const size_t values = (tiles * dim < even ? tiles * dim : even > lists * dim ? even : lists * dim) * 2;
     w.places[i] = static_cast<int>(values / dim < 0x7fffffff ? values / dim : 0x7fffffff);
     w.part[i] = o;
@@ -753,12 +761,12 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
   s.n = a.n;
   s.G = a.G;
   s.rank = a.rank;
-  s.chunk_rows = chunk_rows_for(a.n, blocks_of(a.in_dim), 3 * GPU_SMS);
+  s.chunk_rows = chunk_rows_for(a.n, segments, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, STREAM_MOST);
   if (back && ga->out[0]) outer(0, &s);
   cudaError_t e = cudaSuccess;
   if (s.factor || s.vec) e = launch_lowrank_stream(s, (a.n + s.chunk_rows - 1) / s.chunk_rows + segments, st);
   if (e != cudaSuccess || !vectors) return e;
-  SumArgs u = {planes, blocks_of(a.in_dim), vec, a.v, a.off, a.perm, a.n, a.G, a.rank, a.segments > a.G};
+  SumArgs u = {planes, blocks_of(a.in_dim, stream_channels(a.rank)), vec, a.v, a.off, a.perm, a.n, a.G, a.rank, a.segments > a.G};
   e = launch_lowrank_sum(u, st);
   if (e != cudaSuccess) return e;
   if (a.y) {
@@ -777,7 +785,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
     p.G = a.G;
     p.segments = a.segments;
     p.rank = a.rank;
-    p.chunk_rows = chunk_rows_for(a.n, blocks_of(a.out_dim), 4 * GPU_SMS);
+    p.chunk_rows = chunk_rows_for(a.n, a.segments < a.n ? a.segments : a.n, blocks_of(a.out_dim, UP_CHANNELS), (a.rank <= 32 ? 2 : 1) * GPU_SMS, 64, 2048);
     p.skip_none = a.skip_none;
     e = launch_lowrank_up(p, (a.n + p.chunk_rows - 1) / p.chunk_rows + (a.segments < a.n ? a.segments : a.n), st);
     if (e != cudaSuccess) return e;
@@ -831,7 +839,7 @@ int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const voi
   if (rc != EMOE_OK) return rc;
   if (!A || !B || !x || !y) return EMOE_ERR_INVALID_ARG;
   if (!ptr_aligned(A, 16) || !ptr_aligned(B, 16) || !ptr_aligned(x, 16) || !ptr_aligned(base, 16) || !ptr_aligned(y, 16) ||
-      !ptr_aligned(scales, 4) || !ptr_aligned(out_v, 4))
+      !ptr_aligned(scales, 4) || !ptr_aligned(out_v, 16))
     return EMOE_ERR_ALIGNMENT;
   if (!ctx) return EMOE_ERR_INVALID_ARG;
   const CallScope scope(ctx);
@@ -883,7 +891,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   if (!dy || (!dx && !dA && !dB)) return EMOE_ERR_INVALID_ARG;
   if (((dx || dA) && !B) || (dx && !A) || (dA && !x) || (dB && !v)) return EMOE_ERR_INVALID_ARG;
   if (!ptr_aligned(A, 16) || !ptr_aligned(B, 16) || !ptr_aligned(x, 16) || !ptr_aligned(dy, 16) || !ptr_aligned(dx_base, 16) || !ptr_aligned(dx, 16) ||
-      !ptr_aligned(dA, 16) || !ptr_aligned(dB, 16) || !ptr_aligned(scales, 4) || !ptr_aligned(v, 4))
+      !ptr_aligned(dA, 16) || !ptr_aligned(dB, 16) || !ptr_aligned(scales, 4) || !ptr_aligned(v, 16))
     return EMOE_ERR_ALIGNMENT;
   if (!ctx) return EMOE_ERR_INVALID_ARG;
   size_t have = 0;

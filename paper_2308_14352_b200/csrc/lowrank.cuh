@@ -12,6 +12,13 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// d = a . b, nothing added
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 // Two fp32 values as N pairs of bf16 parts, largest first.  All parts but the last are truncated: what is left is exact, so three
 // parts are the value itself.  An infinity has no rest.
 template <int N>
@@ -69,7 +76,7 @@ __device__ __forceinline__ bool find_chunk(const int32_t* __restrict__ off, int 
     return max(min(off[i + 1], n) - *begin, 0);
   };
   int begin = 0, rows = 0, last_begin = 0, last_rows = 0;
-  if (tid < segments) rows = segment(tid, &begin);
+  if (tid < min(segments, LR_THREADS)) rows = segment(tid, &begin);
   if (segments > LR_THREADS) last_rows = segment(LR_THREADS, &last_begin);  // a 257th segment: beside 256 adapters
   const int chunks = (rows + chunk_rows - 1) / chunk_rows, several = chunks > 1 && tid < G ? chunks : 0;
   int i0 = chunks, i1 = several;
@@ -81,7 +88,7 @@ __device__ __forceinline__ bool find_chunk(const int32_t* __restrict__ off, int 
       i1 += u1;
     }
   }
-  if (lane == 31) {
+  if (lane == 31 && warp < LR_WARPS) {  // (more threads than that have no segment)
     s_scan[warp] = i0;
     s_scan[LR_WARPS + warp] = i1;
   }
@@ -113,7 +120,11 @@ __device__ __forceinline__ bool find_chunk(const int32_t* __restrict__ off, int 
 
 // ---- many bf16 rows (lowrank_stream.cu) --------------------------------------------------------
 
-constexpr int ST_CHANNELS = 64 * LR_WARPS;  // channels of a CTA
+constexpr int UP_CHANNELS = 64 * LR_WARPS;  // channels of a CTA of the up kernel
+// ... of the stream kernel: as many as tensor memory has room for, beside the low-rank vectors
+__host__ __device__ constexpr int stream_channels(int rank) { return rank <= 32 ? 512 : 256; }
+constexpr int STREAM_ROWS = 128;             // rows of its tiles
+constexpr int STREAM_MOST = 1024;            // most rows of a chunk: also how many products it adds in tensor memory before they are rounded properly
 
 struct StreamArgs {
   const __nv_bfloat16* act;     // rows that go by
@@ -121,7 +132,7 @@ struct StreamArgs {
   int dim;                      // values per row, a multiple of 8
   const __nv_bfloat16* factor;  // down factor, [rank][dim] or (by_channel) [dim][rank]; null: no low-rank vectors
   int by_channel;
-  float* planes;                // [blocks of 512 channels][n][rank], by place in the order: shares of the low-rank vectors
+  float* planes;                // [blocks of stream_channels][n][rank], by place in the order: shares of the low-rank vectors
   const float* vec;             // vectors of the outer products, [..][rank]; null: none
   int vec_by_place;             // by place in the order, else by row
   const float* scales;          // of the vectors; null: 1

@@ -3,11 +3,15 @@
 //           tiles, the outer products with the vectors of the other side, dB = s sum dy v^T (dA = sum dv x^T)
 //   sum     the shares of the vectors, one per 512 channels, added in order
 //   up      y = base + s B v (dx = dx_base + A^T s dv)
-// A CTA owns 512 channels of a chunk of one adapter's rows, a warp 64 of them.  Its part of the factor, or of the outer
-// products, stays in registers for all rows of the chunk, and the rows come as tiles of 16 x 64 values through a ring of its own in
-// shared memory that cp.async fills some stages ahead: no wait among the warps for data, and memory latency costs no registers.
-// The tiles are swizzled so that ldmatrix reads them both ways (rows for v, columns for the outer products) without bank conflicts.
+// stream: a value of x takes part in 16 to 64 multiply-adds of v and three times as many of the outer products, too much for the
+// instructions that registers feed once the rank is 32 or 64, so its tiles go from cp.async (rows of any order) to tcgen05 and both sums
+// stay in tensor memory; no thread touches a value of x.  A CTA owns 512 (256) channels of a chunk of one adapter's rows.
+// up: every value of base meets an fp32 sum in a register anyway, so the product is mma.sync there: a warp owns 64 channels, its part of
+// the factor stays in registers, and base comes as tiles of 16 x 64 values through a ring of its own in shared memory that cp.async
+// fills some stages ahead.
 #include "lowrank.cuh"
+#include "pipe.cuh"
+#include "umma.cuh"
 
 namespace emoe {
 namespace {
@@ -110,31 +114,72 @@ struct Vectors {
   }
 };
 
+// ---- stream -------------------------------------------------------------------------------------
+
+// Roles: warps 0-3 bring the factor and the vectors into shared memory as operands and carry results out of tensor memory, warps 4-7
+// copy the rows, warp 8 issues the products.
+constexpr int SK_THREADS = 288, SK_SIDE = 128, SK_STAGES = 4;
+constexpr int SK_TILE = STREAM_ROWS * 128, SK_STAGE = 2 * SK_TILE;  // 128 rows x 64 values; a stage: 128 channels
+
 template <int RT>
 struct Stream {
-  static constexpr int RP = RT * 16, ROWS = RT == 4 ? 16 : 32;  // rows between two meetings of the warps
-  static constexpr int STAGES = 4;
-  using Vec = Vectors<RT, 3, ROWS>;
-  static constexpr int SUM_FLOATS = LR_WARPS * ROWS * RP;
-  static constexpr size_t smem(bool down, bool outer, int chunk_rows) {
-    return static_cast<size_t>(LR_WARPS) * STAGES * TILE_BYTES + (down ? sizeof(float) * SUM_FLOATS : 0) + (outer ? 2 * Vec::BYTES : 0) +
-           sizeof(int) * chunk_rows;
+  static constexpr int RP = RT * 16, CHANNELS = stream_channels(RP), PAIRS = CHANNELS / 128;
+  static constexpr int FACTOR = CHANNELS / 64 * RP * 128;      // [rank][channels], K-major tiles of 64 channels
+  static constexpr int VEC = 2 * 3 * RP * 128;                 // [three parts of rank][128 rows], K-major tiles of 64 rows
+  static constexpr int VEC_BUFS = RT == 4 ? 1 : 2;
+  static constexpr int COL_OUTER = 2 * RP, COLS = COL_OUTER + PAIRS * 3 * RP, TMEM = COLS <= 256 ? 256 : 512;
+  static_assert(COLS <= 512, "tensor memory has 512 columns");
+  static constexpr size_t smem(bool down, bool outer) {
+    return 1024 + static_cast<size_t>(SK_STAGES) * SK_STAGE + (down ? FACTOR : 0) + (outer ? VEC_BUFS * VEC : 0) + sizeof(int) * STREAM_MOST;
   }
 };
-constexpr int ST_MAX_CHUNK = 2048;  // rows listed in shared memory
 
+// byte of value `k` of row `n` in K-major tiles of 64 values, `rows` rows each
+__device__ __forceinline__ uint32_t kmajor_at(int n, int k, int rows) {
+  return k / 64 * rows * 128 + n * 128 + ((k % 64 / 8 ^ (n & 7)) << 4) + k % 8 * 2;
+}
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// The products, for a tile X of 128 rows x 128 channels (two swizzled tiles of 64, as cp.async leaves them):
+//   vectors [128 rows][rank]              += X F^T          X read along its rows (K-major), 16 channels per instruction
+//   outer   [128 channels][3 x rank]      += X^T V          X read along its columns (MN-major), 16 rows per instruction
+// V are the rows' vectors in three bf16 parts side by side, so that the three products cost one instruction; they are added at the
+// end.  Both sums stay in tensor memory: the vectors over the CTA's channels, the outer products over its rows.  The tensor cores cut
+// what they add: over the at most 1024 rows of a chunk that costs a relative 2^-20.
 template <int RT, bool DOWN, bool OUTER>
-__global__ void __launch_bounds__(LR_THREADS, RT == 1 ? 2 : 1) lowrank_stream_kernel(StreamArgs a) {
+__global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArgs a) {
   using S = Stream<RT>;
-  using Vec = typename S::Vec;
-  constexpr int RP = S::RP, ROWS = S::ROWS, NR = 2 * RT;
-  extern __shared__ __align__(128) char smem[];
-  char* s_ring = smem;
-  float* s_sum = reinterpret_cast<float*>(smem + LR_WARPS * S::STAGES * TILE_BYTES);  // [warp][row][rank]
-  char* s_vec = reinterpret_cast<char*>(s_sum + (DOWN ? S::SUM_FLOATS : 0));
-  int* s_rows = reinterpret_cast<int*>(s_vec + (OUTER ? 2 * Vec::BYTES : 0));
+  constexpr int RP = S::RP, PAIRS = S::PAIRS;
+  extern __shared__ char smem_raw[];
+  __shared__ __align__(8) uint64_t bars[2 * SK_STAGES + 10];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int wait_words[PIPE_WORDS];
   __shared__ int s_scan[CHUNK_SCAN];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
+  volatile int* abort_flag = wait_words + PIPE_ABORT;
+  char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  char* s_factor = smem + SK_STAGES * SK_STAGE;
+  char* s_vec = s_factor + (DOWN ? S::FACTOR : 0);
+  int* s_rows = reinterpret_cast<int*>(s_vec + (OUTER ? S::VEC_BUFS * S::VEC : 0));
+  const uint32_t full = smem_u32(bars), empty = full + 8 * SK_STAGES, d1_full = empty + 8 * SK_STAGES, d1_empty = d1_full + 16,
+                 vec_full = d1_empty + 16, vec_empty = vec_full + 16, ready = vec_empty + 16, d2_full = ready + 8;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform_warp();
+  if (tid == 0) {
+    for (int i = 0; i < SK_STAGES; ++i) {
+      mbar_init(full + 8 * i, SK_SIDE);
+      mbar_init(empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(d1_full + 8 * i, 1);
+      mbar_init(d1_empty + 8 * i, SK_SIDE);
+      mbar_init(vec_full + 8 * i, SK_SIDE);
+      mbar_init(vec_empty + 8 * i, 1);
+    }
+    mbar_init(ready, SK_SIDE);
+    mbar_init(d2_full, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    wait_words[PIPE_ABORT] = 0;
+    wait_words[PIPE_FRONT] = 0;
+  }
   pdl_wait();
   pdl_trigger();
   Chunk ch;
@@ -143,171 +188,244 @@ __global__ void __launch_bounds__(LR_THREADS, RT == 1 ? 2 : 1) lowrank_stream_ke
     if (tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
     return;
   }
-  for (int i = tid; i < ch.rows; i += LR_THREADS) s_rows[i] = a.perm ? a.perm[ch.begin + i] : ch.begin + i;
+  for (int i = tid; i < ch.rows; i += SK_THREADS) s_rows[i] = a.perm ? a.perm[ch.begin + i] : ch.begin + i;
+  if (warp == 8) tmem_alloc(smem_u32(&tmem_slot), S::TMEM);
+  tc_fence_before();
   __syncthreads();
-  const int c0 = blockIdx.y * ST_CHANNELS + warp * 64;
-  Ring<S::STAGES> ring;
-  ring.init(s_ring + warp * S::STAGES * TILE_BYTES, a.act, a.stride, c0, a.dim, s_rows, ch.rows);
-  for (int i = 0; i < S::STAGES - 1; ++i) ring.ask(i);
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const int c0 = blockIdx.y * S::CHANNELS, tiles = (ch.rows + STREAM_ROWS - 1) / STREAM_ROWS;
+  const int pairs = min(PAIRS, (a.dim - c0 + 127) / 128);  // of 128 channels; what the last has too many reads as zeros
 
-  // this warp's part of the down factor: [4 x 16 channels][rank in eights], columns are ranks.  by_channel: a word of B holds two
-  // ranks of one channel, so column c of the tiles 2 s and 2 s + 1 is rank 16 s + 2 c and the one behind it.
-  uint32_t down[DOWN ? 4 : 1][NR][2];
-  if constexpr (DOWN) {
-    const uint16_t* f = reinterpret_cast<const uint16_t*>(a.factor) + static_cast<size_t>(ch.adapter) * a.rank * a.dim;
-    const bool even = a.rank % 2 == 0;
+  if (warp >= 4 && warp < 8) {
+    // ---- rows: a thread copies 16 bytes of every eighth row of a tile; rows and channels beyond the end become zeros
+    const int i = tid - 128, piece = i & 15, row0 = i >> 4;
+    const uint32_t dst = smem_u32(smem) + (piece >> 3) * SK_TILE + row0 * 128 + (((piece & 7) ^ row0) << 4);
+    const __nv_bfloat16* row[STREAM_ROWS / 8];
+    uint32_t live = 0;
+    int it = 0;
+    bool ok = true;
+    const auto landed = [&](int stage) {
+      fence_async_proxy();
+      mbar_arrive(full + 8 * (stage % SK_STAGES));
+    };
+    for (int t = 0; t < tiles && ok; ++t) {
+      live = 0;
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
+      for (int j = 0; j < STREAM_ROWS / 8; ++j) {
+        const int at = t * STREAM_ROWS + row0 + 8 * j;
+        if (at < ch.rows) live |= 1u << j;
+        row[j] = a.act + static_cast<size_t>(at < ch.rows ? s_rows[at] : s_rows[0]) * a.stride;
+      }
+      for (int p = 0; p < pairs; ++p, ++it) {
+        const int s = it % SK_STAGES, c = c0 + p * 128 + piece * 8;
+        ok = mbar_wait(empty + 8 * s, ((it / SK_STAGES) & 1) ^ 1, a.check_word, abort_flag);
+        if (!ok) break;
+        const bool inside = c < a.dim;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int c = c0 + kk * 16 + half * 8 + 2 * q;  // two channels
-        if (a.by_channel) {
+        for (int j = 0; j < STREAM_ROWS / 8; ++j) copy_async16(dst + s * SK_STAGE + j * 1024, row[j] + (inside ? c : 0), inside && (live >> j & 1u));
+        copy_commit();
+        copy_wait<SK_STAGES - 1>();
+        if (it >= SK_STAGES - 1) landed(it - (SK_STAGES - 1));
+      }
+    }
+    copy_wait<0>();
+    if (ok)
+      for (int s = max(0, it - (SK_STAGES - 1)); s < it; ++s) landed(s);
+  } else if (warp == 8) {
+    // ---- products
+    const uint32_t on = elect_one();
+    constexpr uint32_t BF16_F32 = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);  // bf16 x bf16 -> fp32, M = 128
+    constexpr uint32_t ID_DOWN = BF16_F32 | (static_cast<uint32_t>(RP / 8) << 17), ID_OUTER = BF16_F32 | (1u << 15) | (static_cast<uint32_t>(3 * RP / 8) << 17);
+    const uint32_t ring = smem_u32(smem), factor = smem_u32(s_factor), vecs = smem_u32(s_vec);
+    bool ok = !DOWN || mbar_wait_warp(ready, 0, a.check_word, abort_flag);
+    int it = 0;
+    for (int t = 0; t < tiles && ok; ++t) {
+      const int buf = t % S::VEC_BUFS;
+      if (OUTER) ok = mbar_wait_warp(vec_full + 8 * buf, (t / S::VEC_BUFS) & 1, a.check_word, abort_flag);
+      if (DOWN && ok) ok = mbar_wait_warp(d1_empty + 8 * (t & 1), ((t >> 1) & 1) ^ 1, a.check_word, abort_flag);
+      for (int p = 0; p < pairs && ok; ++p, ++it) {
+        const int s = it % SK_STAGES;
+        ok = mbar_wait_warp(full + 8 * s, (it / SK_STAGES) & 1, a.check_word, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t stage = ring + s * SK_STAGE;
+        if constexpr (DOWN) {
 #pragma unroll
-          for (int s = 0; s < RT; ++s) {
-            const int r = 16 * s + 2 * g;
-            uint32_t w[2] = {0, 0};
+          for (int k = 0; k < 8; ++k)  // 16 channels each
+            umma_f16_ss_if(on, tmem + (t & 1) * RP, umma_desc(stage + k / 4 * SK_TILE + k % 4 * 32),
+                           umma_desc(factor + (2 * p + k / 4) * RP * 128 + k % 4 * 32), ID_DOWN, p > 0 || k > 0);
+        }
+        if constexpr (OUTER) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-              if (c < a.dim) {
-                const uint16_t* p = f + static_cast<size_t>(c + j) * a.rank + r;
-                if (even) {
-                  if (r < a.rank) w[j] = *reinterpret_cast<const uint32_t*>(p);
-                } else {
-                  if (r < a.rank) w[j] = p[0];
-                  if (r + 1 < a.rank) w[j] |= static_cast<uint32_t>(p[1]) << 16;
-                }
-              }
-            down[kk][2 * s][half] = __byte_perm(w[0], w[1], 0x5410);
-            down[kk][2 * s + 1][half] = __byte_perm(w[0], w[1], 0x7632);
-          }
-        } else {
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            const int r = nr * 8 + g;
-            down[kk][nr][half] = r < a.rank && c < a.dim ? *reinterpret_cast<const uint32_t*>(f + static_cast<size_t>(r) * a.dim + c) : 0u;
-          }
+          for (int k = 0; k < 8; ++k)  // 16 rows each
+            umma_f16_ss_if(on, tmem + S::COL_OUTER + p * 3 * RP, umma_desc_mn(stage + k * 2048, SK_TILE),
+                           umma_desc(vecs + buf * S::VEC + k / 4 * 3 * RP * 128 + k % 4 * 32), ID_OUTER, t > 0 || k > 0);
+        }
+        umma_commit_if(on, empty + 8 * s);
+      }
+      if (!ok) break;
+      if (DOWN) umma_commit_if(on, d1_full + 8 * (t & 1));
+      if (OUTER) umma_commit_if(on, vec_empty + 8 * buf);
+    }
+    if (OUTER && ok) umma_commit_if(on, d2_full);
+  } else if (warp < 4) {
+    bool ok = true;
+    if constexpr (DOWN) {
+      if (a.by_channel) {  // [channels][rank]: a thread turns one channel's ranks at a time
+        for (int c = tid; c < S::CHANNELS; c += SK_SIDE) {
+          const uint16_t* f = reinterpret_cast<const uint16_t*>(a.factor) + (static_cast<size_t>(ch.adapter) * a.dim + c0 + c) * a.rank;
+          const bool inside = c0 + c < a.dim;
+#pragma unroll 16
+          for (int r = 0; r < RP; ++r) *reinterpret_cast<uint16_t*>(s_factor + kmajor_at(r, c, RP)) = inside && r < a.rank ? f[r] : 0;
+        }
+      } else {
+        for (int i = tid; i < RP * S::CHANNELS / 8; i += SK_SIDE) {
+          const int r = i / (S::CHANNELS / 8), c = i % (S::CHANNELS / 8) * 8;
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (r < a.rank && c0 + c < a.dim)
+            w = *reinterpret_cast<const uint4*>(a.factor + (static_cast<size_t>(ch.adapter) * a.rank + r) * a.dim + c0 + c);
+          *reinterpret_cast<uint4*>(s_factor + kmajor_at(r, c, RP)) = w;
         }
       }
-  }
-  const float scale = OUTER && a.scales ? a.scales[ch.adapter] : 1.f;
-  const auto row_of = [&](int i) { return a.vec_by_place ? ch.begin + i : s_rows[i]; };
-  Vec vec;
-  if constexpr (OUTER) {
-    vec.ask(a.vec, a.rank, 0, ch.rows, row_of);
-    vec.put(s_vec, scale);
-  }
-  float acc[OUTER ? 4 : 1][OUTER ? NR : 1][4] = {};
-  int buf = 0;
-  for (int r0 = 0; r0 < ch.rows; r0 += ROWS, buf ^= 1) {
-    __syncthreads();  // the vectors of these rows are there, the sums of those before have been taken
-    if constexpr (OUTER) vec.ask(a.vec, a.rank, r0 + ROWS, ch.rows, row_of);
-    const uint32_t vecs = smem_addr(s_vec + buf * Vec::BYTES);
+      fence_async_proxy();
+      mbar_arrive(ready);
+    }
+    const float scale = OUTER && a.scales ? a.scales[ch.adapter] : 1.f;
+    // vectors of tile t: a thread's row, as a column of the operand
+    const auto put_vectors = [&](int t) {
+      const int buf = t % S::VEC_BUFS, row = t * STREAM_ROWS + tid;
+      const bool live = row < ch.rows;
+      const float* v = a.vec + static_cast<size_t>(live ? (a.vec_by_place ? ch.begin + row : s_rows[row]) : 0) * a.rank;
+      float f[RP];
 #pragma unroll
-    for (int k = 0; k < ROWS / 16; ++k) {
-      const int stage = r0 / 16 + k;
-      if (stage * 16 >= ch.rows) break;
-      const uint32_t tile = ring.get(stage);
-      ring.ask(stage + S::STAGES - 1);
-      if constexpr (DOWN) {
-        float d[NR][4] = {};
+      for (int r = 0; r < RP; r += 4) {
+        if (a.rank % 4 == 0) {
+          const float4 u = live && r < a.rank ? *reinterpret_cast<const float4*>(v + r) : make_float4(0.f, 0.f, 0.f, 0.f);
+          f[r] = u.x; f[r + 1] = u.y; f[r + 2] = u.z; f[r + 3] = u.w;
+        } else {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          uint32_t af[4];
-          ldmatrix4(af, tile + tile_at((lane & 7) + (lane >> 3 & 1) * 8, 2 * kk + (lane >> 4)));
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) mma_bf16(d[nr], af, down[kk][nr][0], down[kk][nr][1]);
+          for (int i = 0; i < 4; ++i) f[r + i] = live && r + i < a.rank ? v[r + i] : 0.f;
         }
-        float* sum = s_sum + (warp * ROWS + k * 16 + g) * RP;
+      }
+      if (!mbar_wait_warp(vec_empty + 8 * buf, ((t / S::VEC_BUFS) & 1) ^ 1, a.check_word, abort_flag)) return false;
 #pragma unroll
-        for (int s = 0; s < RT; ++s) {
-          if (a.by_channel) {  // columns 2 q and 2 q + 1 of both tiles: four neighbouring ranks
-            *reinterpret_cast<float4*>(sum + 16 * s + 4 * q) = make_float4(d[2 * s][0], d[2 * s + 1][0], d[2 * s][1], d[2 * s + 1][1]);
-            *reinterpret_cast<float4*>(sum + 8 * RP + 16 * s + 4 * q) = make_float4(d[2 * s][2], d[2 * s + 1][2], d[2 * s][3], d[2 * s + 1][3]);
-          } else {
+      for (int r = 0; r < RP; r += 2) {
+        uint32_t p[3];
+        split_pair<3>(scale * f[r], scale * f[r + 1], p);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              *reinterpret_cast<float2*>(sum + 16 * s + 8 * h + 2 * q) = make_float2(d[2 * s + h][0], d[2 * s + h][1]);
-              *reinterpret_cast<float2*>(sum + 8 * RP + 16 * s + 8 * h + 2 * q) = make_float2(d[2 * s + h][2], d[2 * s + h][3]);
+        for (int j = 0; j < 3; ++j) {
+          char* base = s_vec + buf * S::VEC;
+          *reinterpret_cast<uint16_t*>(base + kmajor_at(j * RP + r, tid, 3 * RP)) = static_cast<uint16_t>(p[j] & 0xffffu);
+          *reinterpret_cast<uint16_t*>(base + kmajor_at(j * RP + r + 1, tid, 3 * RP)) = static_cast<uint16_t>(p[j] >> 16);
+        }
+      }
+      fence_async_proxy();
+      mbar_arrive(vec_full + 8 * buf);
+      return true;
+    };
+    if constexpr (OUTER) ok = put_vectors(0);
+    for (int t = 0; t < tiles && ok; ++t) {
+      if constexpr (OUTER) {
+        if (t + 1 < tiles && S::VEC_BUFS == 2) ok = put_vectors(t + 1);
+      }
+      if constexpr (DOWN) {
+        if (ok) ok = mbar_wait_warp(d1_full + 8 * (t & 1), (t >> 1) & 1, a.check_word, abort_flag);
+        if (!ok) break;
+        tc_fence_after();
+        const int row = t * STREAM_ROWS + tid;
+        float* plane = a.planes + (static_cast<size_t>(blockIdx.y) * a.n + ch.begin + row) * a.rank;
+#pragma unroll
+        for (int r0 = 0; r0 < RP; r0 += 16) {
+          uint32_t w[16];
+          __syncwarp();
+          tmem_ld16(tmem + (static_cast<uint32_t>(warp * 32) << 16) + (t & 1) * RP + r0, w);
+          tmem_ld_wait();
+          if (row < ch.rows) {
+            if (a.rank % 4 == 0) {
+#pragma unroll
+              for (int i = 0; i < 16; i += 4)
+                if (r0 + i < a.rank) *reinterpret_cast<uint4*>(plane + r0 + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (r0 + i < a.rank) plane[r0 + i] = __uint_as_float(w[i]);
             }
           }
         }
+        tc_fence_before();
+        mbar_arrive(d1_empty + 8 * (t & 1));
       }
       if constexpr (OUTER) {
-        uint32_t vf[3][RT][4];  // two tiles of eight ranks each: b0, b1, b0, b1
-#pragma unroll
-        for (int p = 0; p < 3; ++p)
-#pragma unroll
-          for (int s = 0; s < RT; ++s)
-            ldmatrix4_t(vf[p][s], vecs + (p * ROWS + k * 16 + (lane & 7) + (lane >> 3 & 1) * 8) * Vec::V_BYTES + (2 * s + (lane >> 4)) * 16);
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          uint32_t af[4];
-          ldmatrix4_t(af, tile + tile_at((lane & 7) + (lane >> 4) * 8, 2 * m + (lane >> 3 & 1)));
-#pragma unroll
-          for (int nr = 0; nr < NR; ++nr) {
-            // the tensor cores cut what they add: sixteen rows are summed by themselves, then added with rounding
-            float d[4] = {};
-#pragma unroll
-            for (int p = 2; p >= 0; --p) mma_bf16(d, af, vf[p][nr / 2][nr % 2 * 2], vf[p][nr / 2][nr % 2 * 2 + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][nr][i] += d[i];
-          }
-        }
+        if (t + 1 < tiles && S::VEC_BUFS == 1) ok = put_vectors(t + 1);
       }
     }
-    if constexpr (OUTER) vec.put(s_vec + (buf ^ 1) * Vec::BYTES, scale);
-    if constexpr (DOWN) {
-      __syncthreads();
-      // this CTA's share of the rows' vectors
-      float* plane = a.planes + (static_cast<size_t>(blockIdx.y) * a.n + ch.begin + r0) * a.rank;
-      const int rows = min(ROWS, ch.rows - r0);
-      for (int i = tid; i < rows * RP; i += LR_THREADS) {
-        const int row = i / RP, r = i % RP;
-        float v = 0.f;
+    if constexpr (OUTER) {
+      if (ok) ok = mbar_wait_warp(d2_full, 0, a.check_word, abort_flag);
+      if (ok) {
+        tc_fence_after();
+        const size_t size = static_cast<size_t>(a.dim) * a.rank;
+        float* out = ch.of_adapter == 1 ? a.out + ch.adapter * size : a.part + ch.place * size;
+        for (int p = 0; p < pairs; ++p) {
+          const int c = c0 + p * 128 + tid;
+#pragma unroll 1
+          for (int r0 = 0; r0 < RP; r0 += 16) {
+            uint32_t w[3][16];
+            __syncwarp();
+            const uint32_t at = tmem + (static_cast<uint32_t>(warp * 32) << 16) + S::COL_OUTER + p * 3 * RP + r0;
 #pragma unroll
-        for (int w = 0; w < LR_WARPS; ++w) v += s_sum[w * ROWS * RP + i];
-        if (r < a.rank) plane[row * a.rank + r] = v;
+            for (int j = 0; j < 3; ++j) tmem_ld16(at + j * RP, w[j]);
+            tmem_ld_wait();
+            if (c >= a.dim) continue;
+            float f[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f[i] = (__uint_as_float(w[2][i]) + __uint_as_float(w[1][i])) + __uint_as_float(w[0][i]);
+            if (a.rank_major) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (r0 + i < a.rank) out[static_cast<size_t>(r0 + i) * a.dim + c] = f[i];
+            } else if (a.rank % 4 == 0) {
+#pragma unroll
+              for (int i = 0; i < 16; i += 4)
+                if (r0 + i < a.rank) *reinterpret_cast<float4*>(out + static_cast<size_t>(c) * a.rank + r0 + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (r0 + i < a.rank) out[static_cast<size_t>(c) * a.rank + r0 + i] = f[i];
+            }
+          }
+        }
+        tc_fence_before();
       }
     }
   }
-  if constexpr (OUTER) {
-    const size_t size = static_cast<size_t>(a.dim) * a.rank;
-    float* out = ch.of_adapter == 1 ? a.out + ch.adapter * size : a.part + ch.place * size;
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = c0 + m * 16 + h * 8 + g;
-        if (c >= a.dim) continue;
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const int r = nr * 8 + 2 * q + b;
-            if (r < a.rank) out[a.rank_major ? static_cast<size_t>(r) * a.dim + c : static_cast<size_t>(c) * a.rank + r] = acc[m][nr][2 * h + b];
-          }
-      }
+  __syncthreads();
+  if (warp == 8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, S::TMEM);
   }
 }
 
+// 16, 32 or 64 threads per place, by the rank.
 __global__ void __launch_bounds__(256) lowrank_sum_kernel(SumArgs a) {
   pdl_wait();
   pdl_trigger();
-  const size_t total = static_cast<size_t>(a.n) * a.rank;
-  const size_t i = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= total) return;
-  const int place = static_cast<int>(i / a.rank), r = static_cast<int>(i % a.rank);
+  const int per_cta = a.rank > 32 ? 4 : a.rank > 16 ? 8 : 16, lanes = 256 / per_cta;
+  const int place = blockIdx.x * per_cta + threadIdx.x / lanes, r = threadIdx.x % lanes;
+  if (place >= a.n || r >= a.rank) return;
   const bool mine = place >= a.off[0] && place < a.off[a.G];
   if (!mine && !a.with_none) return;
+  const size_t i = static_cast<size_t>(place) * a.rank + r, plane = static_cast<size_t>(a.n) * a.rank;
   float v = 0.f;
   if (mine) {
 #pragma unroll 8
-    for (int p = 0; p < a.count; ++p) v += a.planes[p * total + i];
+    for (int p = 0; p < a.count; ++p) v += a.planes[p * plane + i];
   }
   a.by_place[i] = v;
   if (a.by_row) a.by_row[static_cast<size_t>(a.perm ? a.perm[place] : place) * a.rank + r] = v;
 }
 
+constexpr int ST_MAX_CHUNK = 2048;  // rows that a CTA lists in shared memory
 template <int RT>
 struct Up {
   static constexpr int ROWS = 64, STAGES = 5;
@@ -335,7 +453,7 @@ __global__ void __launch_bounds__(LR_THREADS, RT == 4 ? 1 : 2) lowrank_up_kernel
   if (ch.adapter < 0 && a.skip_none) return;
   for (int i = tid; i < ch.rows; i += LR_THREADS) s_rows[i] = a.perm ? a.perm[ch.begin + i] : ch.begin + i;
   __syncthreads();
-  const int c0 = blockIdx.y * ST_CHANNELS + warp * 64;
+  const int c0 = blockIdx.y * UP_CHANNELS + warp * 64;
   Ring<U::STAGES> ring;
   ring.init(smem + warp * U::STAGES * TILE_BYTES, a.base, a.stride, c0, a.base ? a.dim : 0, s_rows, ch.rows);
   if (a.base)
@@ -397,7 +515,7 @@ __global__ void __launch_bounds__(LR_THREADS, RT == 4 ? 1 : 2) lowrank_up_kernel
     for (int k = 0; k < U::ROWS / 16; ++k) {
       const int stage = r0 / 16 + k;
       if (stage * 16 >= ch.rows) break;
-      float d[2][4][4] = {};
+      float d[2][4][4];
 #pragma unroll
       for (int s = 0; s < RT; ++s)
 #pragma unroll
@@ -407,7 +525,10 @@ __global__ void __launch_bounds__(LR_THREADS, RT == 4 ? 1 : 2) lowrank_up_kernel
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mma_bf16(d[h][i], vf, up[s][h][i][0], up[s][h][i][1]);
+            for (int i = 0; i < 4; ++i) {
+              if (s == 0 && p == 1) mma_bf16_first(d[h][i], vf, up[s][h][i][0], up[s][h][i][1]);
+              else mma_bf16(d[h][i], vf, up[s][h][i][0], up[s][h][i][1]);
+            }
         }
       uint32_t tile = 0;
       if (a.base) {
@@ -446,10 +567,11 @@ __global__ void __launch_bounds__(LR_THREADS, RT == 4 ? 1 : 2) lowrank_up_kernel
 
 template <int RT, bool DOWN, bool OUTER>
 cudaError_t launch_stream_of(const StreamArgs& a, int chunks, cudaStream_t st) {
-  const cudaError_t e = allow_smem<lowrank_stream_kernel<RT, DOWN, OUTER>>(static_cast<int>(Stream<RT>::smem(DOWN, OUTER, ST_MAX_CHUNK)));
+  constexpr size_t smem = Stream<RT>::smem(DOWN, OUTER);
+  const cudaError_t e = allow_smem<lowrank_stream_kernel<RT, DOWN, OUTER>>(static_cast<int>(smem));
   if (e != cudaSuccess) return e;
-  return launch_chain(lowrank_stream_kernel<RT, DOWN, OUTER>, dim3(chunks, (a.dim + ST_CHANNELS - 1) / ST_CHANNELS), dim3(LR_THREADS),
-                      Stream<RT>::smem(DOWN, OUTER, a.chunk_rows), st, a);
+  return launch_chain(lowrank_stream_kernel<RT, DOWN, OUTER>, dim3(chunks, (a.dim + Stream<RT>::CHANNELS - 1) / Stream<RT>::CHANNELS), dim3(SK_THREADS),
+                      smem, st, a);
 }
 
 template <int RT>
@@ -462,20 +584,20 @@ template <int RT>
 cudaError_t launch_up_rank(const UpArgs& a, int chunks, cudaStream_t st) {
   const cudaError_t e = allow_smem<lowrank_up_kernel<RT>>(static_cast<int>(Up<RT>::smem(ST_MAX_CHUNK)));
   if (e != cudaSuccess) return e;
-  return launch_chain(lowrank_up_kernel<RT>, dim3(chunks, (a.dim + ST_CHANNELS - 1) / ST_CHANNELS), dim3(LR_THREADS), Up<RT>::smem(a.chunk_rows), st, a);
+  return launch_chain(lowrank_up_kernel<RT>, dim3(chunks, (a.dim + UP_CHANNELS - 1) / UP_CHANNELS), dim3(LR_THREADS), Up<RT>::smem(a.chunk_rows), st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_lowrank_stream(const StreamArgs& a, int chunks, cudaStream_t st) {
-  if (a.chunk_rows > ST_MAX_CHUNK) return cudaErrorInvalidValue;
+  if (a.chunk_rows > STREAM_MOST) return cudaErrorInvalidValue;
   if (a.rank <= 16) return launch_stream_rank<1>(a, chunks, st);
   return a.rank <= 32 ? launch_stream_rank<2>(a, chunks, st) : launch_stream_rank<4>(a, chunks, st);
 }
 
 cudaError_t launch_lowrank_sum(const SumArgs& a, cudaStream_t st) {
-  const size_t total = static_cast<size_t>(a.n) * a.rank;
-  return launch_chain(lowrank_sum_kernel, dim3(static_cast<unsigned>((total + 255) / 256)), dim3(256), 0, st, a);
+  const int per_cta = a.rank > 32 ? 4 : a.rank > 16 ? 8 : 16;
+  return launch_chain(lowrank_sum_kernel, dim3((a.n + per_cta - 1) / per_cta), dim3(256), 0, st, a);
 }
 
 cudaError_t launch_lowrank_up(const UpArgs& a, int chunks, cudaStream_t st) {

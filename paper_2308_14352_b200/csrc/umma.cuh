@@ -15,6 +15,13 @@ __device__ __forceinline__ uint64_t umma_desc(uint32_t smem_addr) {
          (1ull << 46) | (2ull << 61);
 }
 
+// The same tile read the other way (MN-major: the 64 values of a row are the operand's rows or columns, the tile's rows the reduction):
+// tiles of 64 values `next_64` bytes apart, 8 rows of the reduction 1024 bytes apart.
+__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t smem_addr, uint32_t next_64) {
+  return static_cast<uint64_t>((smem_addr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(next_64 >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+
 // 8-bit integers -> int32: A from shared memory ...
 __device__ __forceinline__ void umma_i8_ss(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -46,6 +53,15 @@ __device__ __forceinline__ void umma_f16_ts_if(uint32_t on, uint32_t d_tmem, uin
       "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
       :
       : "r"(d_tmem), "r"(a_tmem), "l"(db), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+// A and B from shared memory, both of the 16-bit type that the instruction descriptor names
+__device__ __forceinline__ void umma_f16_ss_if(uint32_t on, uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      :
+      : "r"(d_tmem), "l"(da), "l"(db), "r"(idesc), "r"(accumulate), "r"(on)
       : "memory");
 }
 __device__ __forceinline__ void umma_commit_if(uint32_t on, uint32_t bar) {
