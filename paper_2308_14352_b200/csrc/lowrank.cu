@@ -463,9 +463,9 @@ __global__ void __launch_bounds__(LR_THREADS, RT * NT <= 8 && sizeof(T) == 2 ? 2
 // ---- gradients of the factors -------------------------------------------------------------------
 
 // out[c][r] = sum over an adapter's rows of act[row][c] vec[row][r]:  dB from dy and s v (out [N][rank]), dA from x and dv (out [rank][K]).
-// The reduction runs over rows, so a lane takes the same eight channels of four rows and interleaves pairs of rows.  A CTA owns a chunk
-// of an adapter's rows and 64 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
-// parts.  An adapter whose rows are one chunk is written at once, else its chunks' shares are joined behind this kernel in order.
+// The reduction runs over rows, so a lane takes the same eight channels of four rows and interleaves pairs of rows.  A CTA owns an even
+// run of the rows and 64 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
+// parts.  A segment that is one run's alone is written at once, else the runs' shares are joined behind this kernel, in order.
 constexpr int GR_ROWS = 64, GR_CHANNELS = 64 * LR_WARPS;
 
 struct GradArgs {
@@ -476,36 +476,33 @@ struct GradArgs {
   float* out[2];          // dB, dA (null: not wanted)
   const float* scales;    // of dB
   const int32_t *off, *perm;
-  float* part[2];         // [chunks of adapters with several][dim][rank]
-  int* check_word;
-  int n, G, rank, chunk_rows[2], blocks[2], places[2];
+  float* part[2];         // [2 x runs][dim][rank]: shares of segments that several runs have
+  int n, G, rank, runs[2], blocks[2];
 };
 
 template <typename T, int RT>
 __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a) {
   constexpr int NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
   __shared__ uint32_t s_vec[3][PAIRS][W_STRIDE];
-  __shared__ int s_rows[GR_ROWS], s_scan[CHUNK_SCAN];
+  __shared__ int s_rows[GR_ROWS];
+  __shared__ TileList list;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
   pdl_wait();
   pdl_trigger();
   const int which = static_cast<int>(blockIdx.y) >= a.blocks[0], block = blockIdx.y - (which ? a.blocks[0] : 0);
-  Chunk ch;
-  if (!find_chunk(a.off, a.G, a.G, a.n, a.chunk_rows[which], blockIdx.x, s_scan, &ch)) return;
-  if (ch.of_adapter > 1 && ch.place >= a.places[which]) {  // only where the segments overlap
-    if (tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
-    return;
-  }
+  if (static_cast<int>(blockIdx.x) >= a.runs[which]) return;
+  const TileRun run = list_tiles<GR_ROWS>(list, a.off, a.G, a.n, blockIdx.x, a.runs[which]);
+  if (run.lo >= run.hi) return;
   const int dim = a.dim[which], c0 = block * GR_CHANNELS + warp * 64 + 8 * g;  // this lane's eight channels
   const T* act = static_cast<const T*>(a.act[which]);
   const float* vec = a.vec[which];
-  const float scale = which == 0 && a.scales ? a.scales[ch.adapter] : 1.f;
   float acc[4][NR][4] = {};
-  for (int r0 = 0; r0 < ch.rows; r0 += GR_ROWS) {
-    const int rows = min(GR_ROWS, ch.rows - r0);
+  for (int t = run.lo, segment = list.segment; t < run.hi; ++t) {
+    const Tile tile = tile_of<GR_ROWS>(list, run, t, &segment);
+    const int rows = tile.rows;
+    const float scale = which == 0 && a.scales ? a.scales[segment] : 1.f;
     __syncthreads();  // the vectors of the rows before have been used
-    for (int i = tid; i < GR_ROWS; i += LR_THREADS)
-      s_rows[i] = i < rows ? (a.perm ? a.perm[ch.begin + r0 + i] : ch.begin + r0 + i) : -1;
+    for (int i = tid; i < GR_ROWS; i += LR_THREADS) s_rows[i] = i < rows ? (a.perm ? a.perm[tile.begin + i] : tile.begin + i) : -1;
     __syncthreads();
     for (int i = tid; i < PAIRS * RP; i += LR_THREADS) {
       const int pair = i / RP, r = i % RP, ra = s_rows[2 * pair], rb = s_rows[2 * pair + 1];
@@ -564,59 +561,51 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
         }
       }
     }
-  }
-  if (c0 >= dim) return;
-  const size_t size = static_cast<size_t>(dim) * a.rank;
-  float* out = ch.of_adapter == 1 ? a.out[which] + ch.adapter * size : a.part[which] + ch.place * size;
-  // c0 + 2 m + h, rank nr * 8 + 2 q + b
+    if (!tile.ends) continue;
+    const size_t size = static_cast<size_t>(dim) * a.rank;
+    const int share = share_of(list, run, segment, blockIdx.x);
+    float* out = share < 0 ? a.out[which] + segment * size : a.part[which] + share * size;
+    // c0 + 2 m + h, rank nr * 8 + 2 q + b
 #pragma unroll
-  for (int nr = 0; nr < NR; ++nr)
+    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int r = nr * 8 + 2 * q + b;
-      if (r >= a.rank) continue;
-      if (which == 0) {
+      for (int b = 0; b < 2; ++b) {
+        const int r = nr * 8 + 2 * q + b;
+        if (r >= a.rank || c0 >= dim) continue;
+        if (which == 0) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) out[static_cast<size_t>(c0 + c) * a.rank + r] = acc[c / 2][nr][2 * (c % 2) + b];
-      } else {
-        float4* o = reinterpret_cast<float4*>(out + static_cast<size_t>(r) * dim + c0);
-        o[0] = make_float4(acc[0][nr][b], acc[0][nr][2 + b], acc[1][nr][b], acc[1][nr][2 + b]);
-        o[1] = make_float4(acc[2][nr][b], acc[2][nr][2 + b], acc[3][nr][b], acc[3][nr][2 + b]);
+          for (int c = 0; c < 8; ++c) out[static_cast<size_t>(c0 + c) * a.rank + r] = acc[c / 2][nr][2 * (c % 2) + b];
+        } else {
+          float4* o = reinterpret_cast<float4*>(out + static_cast<size_t>(r) * dim + c0);
+          o[0] = make_float4(acc[0][nr][b], acc[0][nr][2 + b], acc[1][nr][b], acc[1][nr][2 + b]);
+          o[1] = make_float4(acc[2][nr][b], acc[2][nr][2 + b], acc[3][nr][b], acc[3][nr][2 + b]);
+        }
       }
-    }
+#pragma unroll
+    for (int i = 0; i < 4 * NR * 4; ++i) (&acc[0][0][0])[i] = 0.f;
+  }
 }
 
-// Joins the chunks of adapters with several, in order, and clears the gradients of adapters without rows.  grid: (adapters, shares of a
-// gradient, dB and dA)
+// Joins the shares of segments that several runs have, in order, and clears the gradients of adapters without rows.  grid: (adapters,
+// pieces of a gradient, dB and dA); H: rows of a tile of the kernel in front.
+template <int H>
 __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
-  __shared__ int s_scan[LR_WARPS + 1];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, adapter = blockIdx.x, which = blockIdx.z;
+  __shared__ TileList list;
+  const int tid = threadIdx.x, adapter = blockIdx.x, which = blockIdx.z;
   pdl_wait();
   pdl_trigger();
   if (!a.out[which]) return;
-  int several = 0, chunks = 0;
-  if (tid < a.G) {
-    const int begin = min(max(a.off[tid], 0), a.n), rows = max(min(a.off[tid + 1], a.n) - begin, 0);
-    chunks = (rows + a.chunk_rows[which] - 1) / a.chunk_rows[which];
-    several = chunks > 1 ? chunks : 0;
-  }
-  const int front = __reduce_add_sync(0xffffffffu, tid < adapter ? several : 0);
-  if (lane == 0) s_scan[warp] = front;
-  if (tid == adapter) s_scan[LR_WARPS] = chunks;
-  __syncthreads();
-  const int mine = s_scan[LR_WARPS];
-  if (mine == 1) return;
-  int place = 0;
-  for (int w = 0; w < LR_WARPS; ++w) place += s_scan[w];
-  if (mine > 1 && place + mine > a.places[which]) return;
+  const TileRun run = list_tiles<H>(list, a.off, a.G, a.n, 0, a.runs[which]);
+  const int first = list.first[adapter], end = list.first[adapter + 1], c0 = first / run.per, c1 = end > first ? (end - 1) / run.per : c0 - 1;
+  if (c0 == c1) return;
   const size_t words = static_cast<size_t>(a.dim[which]) * a.rank / 4;  // dim is a multiple of 8
   float4* out = reinterpret_cast<float4*>(a.out[which]) + adapter * words;
-  const float4* in = reinterpret_cast<const float4*>(a.part[which]) + place * words;
+  const float4* in = reinterpret_cast<const float4*>(a.part[which]);
   for (size_t i = static_cast<size_t>(blockIdx.y) * LR_THREADS + tid; i < words; i += static_cast<size_t>(gridDim.y) * LR_THREADS) {
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int c = 0; c < mine; ++c) {
-      const float4 u = in[c * words + i];
+    for (int c = c0; c <= c1; ++c) {
+      const float4 u = in[(2 * c + (c < c1)) * words + i];
       s.x += u.x; s.y += u.y; s.z += u.z; s.w += u.w;
     }
     out[i] = s;
@@ -630,47 +619,41 @@ constexpr int LR_STREAM_ROWS = 512;
 
 struct LowrankLayout {
   size_t off, perm, vec, planes, part[2], total;  // vec: dv, or the vectors in the order; planes: their shares
-  int chunk_rows[2], chunks[2], places[2];        // of the gradients: dB, dA
+  int runs[2];                                    // of the outer products: dB, dA
 };
 
-// Rows per chunk of the kernels on many rows, for `blocks` CTAs per chunk where the GPU holds `slots` at once: the fewest rows with which
-// all CTAs run side by side (a few left over would take as long again), a segment's last chunk counted as whole.  Many segments
-// make several rounds of CTAs whatever the chunks: then twice the mean segment, so that a long one is shared out.
-int chunk_rows_for(int n, int segments, int blocks, int slots, int tile, int most) {
-  const int chunks = slots / blocks - segments, mean = (n + segments - 1) / segments;
-  int rows = chunks > 0 ? (n + chunks - 1) / chunks : 2 * mean > 256 ? 2 * mean : 256;
-  if (rows > most) rows = most;
-  return (rows + tile - 1) / tile * tile;
-}
 int blocks_of(int dim, int channels) { return (dim + channels - 1) / channels; }
+// Even runs of the rows, for `blocks` CTAs per run where the GPU holds `slots` at once: as many as run side by side, or whole multiples
+// of that where a run would be longer than `most` tiles.
+int runs_for(int n, int segments, int blocks, int slots, int tile, int most) {
+  const int side = slots / blocks > 0 ? slots / blocks : 1, tiles = (n + tile - 1) / tile + (segments < n ? segments : n);
+  const int least = (tiles + most - 1) / most, runs = (least + side - 1) / side * side;
+  return runs < tiles ? runs : tiles;
+}
 bool takes_stream(const emoe_lowrank_desc& D, int n) { return D.dtype == EMOE_DTYPE_BF16 && n > LR_STREAM_ROWS; }
 
 LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
   const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+  const bool stream = takes_stream(D, n);
   LowrankLayout w{};
-  const int segments = D.n_adapters < n ? D.n_adapters : n;
   const size_t vectors = sizeof(float) * static_cast<size_t>(n) * D.rank;
   size_t o = 0;
   w.off = o;  o += up(sizeof(int32_t) * (D.n_adapters + 2));
   w.perm = o; o += up(sizeof(int32_t) * static_cast<size_t>(n));
   w.vec = o;  o += up(vectors);
   w.planes = o;
-  const bool stream = takes_stream(D, n);
-  const int channels = stream ? stream_channels(D.rank) : GR_CHANNELS;
-  if (stream) o += up(vectors * blocks_of(D.in_dim > D.out_dim ? D.in_dim : D.out_dim, channels));
+  if (stream) o += up(vectors * blocks_of(D.in_dim > D.out_dim ? D.in_dim : D.out_dim, stream_channels(D.rank)));
   for (int i = 0; i < 2; ++i) {
-    const int dim = i ? D.in_dim : D.out_dim, blocks = blocks_of(dim, channels);
-    w.chunk_rows[i] = chunk_rows_for(n, segments, blocks, GPU_SMS, stream ? STREAM_ROWS : GR_ROWS, STREAM_MOST);
-    w.chunks[i] = (n + w.chunk_rows[i] - 1) / w.chunk_rows[i];
-    // An adapter with several chunks fills all of them but one, so that there are no more than twice as many of those as all rows together
-    // make: n over the rows of a chunk, which are slots / blocks of all or more, 1024 at most, or twice the mean segment.  The room for them
-    // grows with n, dim and rank alike (slots / blocks * dim <= slots * channels), so that a context that is made for the largest call serves all.
-    const size_t tiles = (n + 63) / 64, lists = (n + STREAM_MOST - 1) / STREAM_MOST, by_mean = (segments + 1) / 2 + 1;
-    const size_t even = static_cast<size_t>(GPU_SMS) * 512 + (by_mean + 1) * dim;
-    const size_t values = (tiles * dim < even ? tiles * dim : even > lists * dim ? even : lists * dim) * 2;
-    w.places[i] = static_cast<int>(values / dim < 0x7fffffff ? values / dim : 0x7fffffff);
+    const size_t dim = i ? D.in_dim : D.out_dim;
+    // 1024 rows at most per run, as accuracy goes on the streaming path
+    w.runs[i] = runs_for(n, D.n_adapters, blocks_of(static_cast<int>(dim), stream ? stream_channels(D.rank) : GR_CHANNELS), GPU_SMS,
+                         stream ? STREAM_ROWS : GR_ROWS, stream ? STREAM_RUN : STREAM_RUN * STREAM_ROWS / GR_ROWS);
     w.part[i] = o;
-    o += up(sizeof(float) * values * D.rank);
+    // Two shares per run.  What is reserved grows with n, dim and rank alike, so that a context that is made for the largest call serves all:
+    // runs <= slots / blocks + tiles / 8 + 1 and slots / blocks * dim <= slots * 512; runs <= tiles.
+    const size_t tiles = (static_cast<size_t>(n) + 63) / 64 + (D.n_adapters < n ? D.n_adapters : n);
+    const size_t even = static_cast<size_t>(2 * GPU_SMS) * 512 + (tiles / 8 + 2) * dim;
+    o += up(sizeof(float) * 2 * (tiles * dim < even ? tiles * dim : even) * D.rank);
   }
   w.total = o;
   return w;
@@ -719,14 +702,16 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
   return by_rows(std::integral_constant<int, 4>());
 }
 
-cudaError_t launch_join(const GradArgs& a, cudaStream_t st) {
+cudaError_t launch_join(const GradArgs& a, bool stream, cudaStream_t st) {
   const size_t dim = a.dim[0] > a.dim[1] ? a.dim[0] : a.dim[1], shares = (dim * a.rank / 4 + LR_THREADS - 1) / LR_THREADS;
-  return launch_chain(lowrank_join_kernel, dim3(a.G, static_cast<unsigned>(shares < 32 ? shares : 32), 2), dim3(LR_THREADS), 0, st, a);
+  const dim3 grid(a.G, static_cast<unsigned>(shares < 32 ? shares : 32), 2);
+  if (stream) return launch_chain(lowrank_join_kernel<STREAM_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
+  return launch_chain(lowrank_join_kernel<GR_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
 }
 
 template <typename T>
-cudaError_t launch_grads(const GradArgs& a, int chunks, cudaStream_t st) {
-  const dim3 grid(chunks, a.blocks[0] + a.blocks[1]);
+cudaError_t launch_grads(const GradArgs& a, cudaStream_t st) {
+  const dim3 grid(a.runs[0] > a.runs[1] ? a.runs[0] : a.runs[1], a.blocks[0] + a.blocks[1]);
   if (a.rank <= 16) return launch_chain(lowrank_grad_kernel<T, 1>, grid, dim3(LR_THREADS), 0, st, a);
   if (a.rank <= 32) return launch_chain(lowrank_grad_kernel<T, 2>, grid, dim3(LR_THREADS), 0, st, a);
   return launch_chain(lowrank_grad_kernel<T, 4>, grid, dim3(LR_THREADS), 0, st, a);
@@ -735,7 +720,6 @@ cudaError_t launch_grads(const GradArgs& a, int chunks, cudaStream_t st) {
 // Many bf16 rows: rows that go down and, backward, the outer products; the vectors' sum; rows that come up.
 cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, char* ws, const LowrankLayout& w, cudaStream_t st) {
   using bf16 = __nv_bfloat16;
-  const int segments = a.G < a.n ? a.G : a.n;
   float *vec = reinterpret_cast<float*>(ws + w.vec), *planes = reinterpret_cast<float*>(ws + w.planes);
   const bool vectors = a.y || a.v || (back && ga->out[1]);
   const auto outer = [&](int which, StreamArgs* s) {
@@ -745,8 +729,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
     s->out = ga->out[which];
     s->part = ga->part[which];
     s->rank_major = which;
-    s->chunk_rows = w.chunk_rows[which];
-    s->places = w.places[which];
+    s->runs = w.runs[which];
   };
   StreamArgs s = {};
   s.act = static_cast<const bf16*>(a.x);
@@ -761,10 +744,10 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
   s.n = a.n;
   s.G = a.G;
   s.rank = a.rank;
-  s.chunk_rows = chunk_rows_for(a.n, segments, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, STREAM_MOST);
+  s.runs = runs_for(a.n, a.G, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, STREAM_RUN);
   if (back && ga->out[0]) outer(0, &s);
   cudaError_t e = cudaSuccess;
-  if (s.factor || s.vec) e = launch_lowrank_stream(s, (a.n + s.chunk_rows - 1) / s.chunk_rows + segments, st);
+  if (s.factor || s.vec) e = launch_lowrank_stream(s, st);
   if (e != cudaSuccess || !vectors) return e;
   SumArgs u = {planes, blocks_of(a.in_dim, stream_channels(a.rank)), vec, a.v, a.off, a.perm, a.n, a.G, a.rank, a.segments > a.G};
   e = launch_lowrank_sum(u, st);
@@ -785,9 +768,9 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
     p.G = a.G;
     p.segments = a.segments;
     p.rank = a.rank;
-    p.chunk_rows = chunk_rows_for(a.n, a.segments < a.n ? a.segments : a.n, blocks_of(a.out_dim, UP_CHANNELS), (a.rank <= 32 ? 2 : 1) * GPU_SMS, 64, 2048);
+    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, UP_CHANNELS), (a.rank <= 32 ? 2 : 1) * GPU_SMS, UP_ROWS, UP_RUN);
     p.skip_none = a.skip_none;
-    e = launch_lowrank_up(p, (a.n + p.chunk_rows - 1) / p.chunk_rows + (a.segments < a.n ? a.segments : a.n), st);
+    e = launch_lowrank_up(p, st);
     if (e != cudaSuccess) return e;
   }
   if (!back || !ga->out[1]) return cudaSuccess;
@@ -797,7 +780,8 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
   x.dim = ga->dim[1];
   x.factor = nullptr;
   outer(1, &x);
-  return launch_lowrank_stream(x, w.chunks[1] + segments, st);
+  x.early = 1;  // behind the sum of the vectors or the kernel that takes them up
+  return launch_lowrank_stream(x, st);
 }
 
 int check_lowrank(const emoe_lowrank_desc* D, int n, const int32_t* ids, const int32_t* off) {
@@ -941,26 +925,22 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   ga.scales = scales;
   ga.off = a.off;
   ga.perm = a.perm;
-  ga.check_word = a.check_word;
   ga.n = n;
   ga.G = desc->n_adapters;
   ga.rank = desc->rank;
   for (int i = 0; i < 2; ++i) {
     ga.part[i] = reinterpret_cast<float*>(ws + w.part[i]);
     ga.blocks[i] = ga.out[i] ? (ga.dim[i] + GR_CHANNELS - 1) / GR_CHANNELS : 0;
-    ga.chunk_rows[i] = w.chunk_rows[i];
-    ga.places[i] = w.places[i];
+    ga.runs[i] = w.runs[i];
   }
-  const int none_or_one = ga.G < n ? ga.G : n;  // segments that do not end on a chunk's end
   if (takes_stream(*desc, n)) {
     EMOE_CALL(ctx, launch_many(a, true, &ga, ws, w, st));
   } else {
     const bool bf16 = desc->dtype == EMOE_DTYPE_BF16;
     if (dx || dA) EMOE_CALL(ctx, bf16 ? (launch_lowrank<__nv_bfloat16, true>(a, st)) : (launch_lowrank<float, true>(a, st)));
-    const int chunks = (w.chunks[0] > w.chunks[1] ? w.chunks[0] : w.chunks[1]) + none_or_one;
-    if (dA || dB) EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, chunks, st) : launch_grads<float>(ga, chunks, st));
+    if (dA || dB) EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, st) : launch_grads<float>(ga, st));
   }
-  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, st));
+  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, takes_stream(*desc, n), st));
   return EMOE_OK;
 }
 

@@ -60,62 +60,77 @@ __device__ __forceinline__ uint4 load16(const void* p) {
 }
 __device__ __forceinline__ uint4 load16_keep(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
-// A run of one adapter's rows: adapter (-1: the rows of no adapter), first place in the order and rows, the number of its
-// adapter's chunks and its place among the chunks of adapters with several.
-struct Chunk {
-  int adapter, begin, rows, of_adapter, place;
+// ---- rows shared out evenly ----------------------------------------------------------------------
+// The rows of every segment (the G adapters and, where there is one more, the rows of none) make tiles of H rows, the last of a
+// segment with fewer; the tiles of all segments, one behind the other, are cut into even runs, one per CTA.  A run may begin and end
+// inside a segment.
+constexpr int MAX_SEGMENTS = EMOE_MAX_EXPERTS + 1;
+struct TileList {
+  int first[MAX_SEGMENTS + 1];  // of a segment's tiles; behind the last: their number
+  int begin[MAX_SEGMENTS];      // of its rows, in the order
+  int rows[MAX_SEGMENTS];
+  int scan[LR_WARPS];
+  int segment;                  // of the CTA's first tile
 };
-constexpr int CHUNK_SCAN = 2 * LR_WARPS + 5;
+struct TileRun {
+  int lo, hi, per;  // tiles of this CTA; of every CTA but the last
+};
 
-// Chunk `c` of the list of all segments' chunks of `chunk_rows` rows; false: no such chunk.  Segments: the G adapters and, where there is
-// one more, the rows of none.  Every thread of the CTA calls it; s_scan: CHUNK_SCAN words.
-__device__ __forceinline__ bool find_chunk(const int32_t* __restrict__ off, int segments, int G, int n, int chunk_rows, int c, int* s_scan, Chunk* out) {
+// Fills the list and gives run `cta` of `ctas`.  Every thread of the CTA calls it (at least LR_THREADS).
+template <int H>
+__device__ __forceinline__ TileRun list_tiles(TileList& list, const int32_t* __restrict__ off, int segments, int n, int cta, int ctas) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const auto segment = [&](int i, int* begin) {
-    *begin = min(max(off[i], 0), n);
-    return max(min(off[i + 1], n) - *begin, 0);
+  const auto segment = [&](int i) {
+    const int begin = min(max(off[i], 0), n), rows = max(min(off[i + 1], n) - begin, 0);
+    list.begin[i] = begin;
+    list.rows[i] = rows;
+    return (rows + H - 1) / H;
   };
-  int begin = 0, rows = 0, last_begin = 0, last_rows = 0;
-  if (tid < min(segments, LR_THREADS)) rows = segment(tid, &begin);
-  if (segments > LR_THREADS) last_rows = segment(LR_THREADS, &last_begin);  // a 257th segment: beside 256 adapters
-  const int chunks = (rows + chunk_rows - 1) / chunk_rows, several = chunks > 1 && tid < G ? chunks : 0;
-  int i0 = chunks, i1 = several;
+  const int tiles = tid < min(segments, LR_THREADS) ? segment(tid) : 0;
+  int last = 0;
+  if (tid == 0 && segments > LR_THREADS) last = segment(LR_THREADS);  // a 257th segment: beside 256 adapters
+  int incl = tiles;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u0 = __shfl_up_sync(0xffffffffu, i0, o), u1 = __shfl_up_sync(0xffffffffu, i1, o);
-    if (lane >= o) {
-      i0 += u0;
-      i1 += u1;
-    }
+    const int u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
   }
-  if (lane == 31 && warp < LR_WARPS) {  // (more threads than that have no segment)
-    s_scan[warp] = i0;
-    s_scan[LR_WARPS + warp] = i1;
-  }
-  int* s = s_scan + 2 * LR_WARPS;
-  if (tid == 0) s[2] = 0;
+  if (lane == 31 && warp < LR_WARPS) list.scan[warp] = incl;
   __syncthreads();
-  int f0 = i0 - chunks, f1 = i1 - several, all = 0;
+  int front = 0, all = 0;
+#pragma unroll
   for (int w = 0; w < LR_WARPS; ++w) {
-    if (w < warp) {
-      f0 += s_scan[w];
-      f1 += s_scan[LR_WARPS + w];
-    }
-    all += s_scan[w];
+    if (w < warp) front += list.scan[w];
+    all += list.scan[w];
   }
-  const auto put = [&](int adapter, int first, int of, int begin_, int rows_, int place) {
-    s[0] = adapter;
-    s[1] = begin_ + (c - first) * chunk_rows;
-    s[2] = min(chunk_rows, rows_ - (c - first) * chunk_rows);
-    s[3] = of;
-    s[4] = place;
-  };
-  if (c >= f0 && c < f0 + chunks) put(tid < G ? tid : -1, f0, chunks, begin, rows, f1 + (c - f0));
-  const int last_chunks = (last_rows + chunk_rows - 1) / chunk_rows;
-  if (tid == 0 && c >= all && c < all + last_chunks) put(-1, all, last_chunks, last_begin, last_rows, 0);
+  if (tid < min(segments, LR_THREADS)) list.first[tid] = front + incl - tiles;
+  if (tid == 0) {
+    list.first[min(segments, LR_THREADS)] = all;
+    if (segments > LR_THREADS) list.first[segments] = all + last;
+  }
   __syncthreads();
-  *out = {s[0], s[1], s[2], s[3], s[4]};
-  return s[2] > 0;
+  const int total = list.first[segments], per = max((total + ctas - 1) / ctas, 1), lo = min(cta * per, total);
+  for (int i = tid; i < segments; i += blockDim.x)
+    if (lo >= list.first[i] && lo < list.first[i + 1]) list.segment = i;
+  __syncthreads();
+  return {lo, min(lo + per, total), per};
+}
+// The tile `t` of a walk along a run: `segment` follows (it starts at list.segment).
+struct Tile {
+  int begin, rows;  // in the order
+  bool starts, ends;  // the first, the last of its segment within the run
+};
+template <int H>
+__device__ __forceinline__ Tile tile_of(const TileList& list, const TileRun& run, int t, int* segment) {
+  while (t >= list.first[*segment + 1]) ++*segment;
+  const int s = *segment, in_segment = (t - list.first[s]) * H;
+  return {list.begin[s] + in_segment, min(H, list.rows[s] - in_segment), t == run.lo || t == list.first[s], t + 1 == run.hi || t + 1 == list.first[s + 1]};
+}
+// Outer products of a segment that several runs share are joined behind the kernel, in order.  Where a run leaves its share of segment
+// s: the part of one that goes on in the next run, else of one that began before; -1: the segment is the run's alone.
+__device__ __forceinline__ int share_of(const TileList& list, const TileRun& run, int s, int cta) {
+  if (list.first[s + 1] > run.hi) return 2 * cta + 1;
+  return list.first[s] < run.lo ? 2 * cta : -1;
 }
 
 // ---- many bf16 rows (lowrank_stream.cu) --------------------------------------------------------
@@ -123,8 +138,8 @@ __device__ __forceinline__ bool find_chunk(const int32_t* __restrict__ off, int 
 constexpr int UP_CHANNELS = 64 * LR_WARPS;  // channels of a CTA of the up kernel
 // ... of the stream kernel: as many as tensor memory has room for, beside the low-rank vectors
 __host__ __device__ constexpr int stream_channels(int rank) { return rank <= 32 ? 512 : 256; }
-constexpr int STREAM_ROWS = 128;             // rows of its tiles
-constexpr int STREAM_MOST = 1024;            // most rows of a chunk: also how many products it adds in tensor memory before they are rounded properly
+constexpr int STREAM_ROWS = 128, STREAM_RUN = 8;  // rows of its tiles; tiles of its longest run: how many products are added in tensor memory
+constexpr int UP_ROWS = 64, UP_RUN = 32;
 
 struct StreamArgs {
   const __nv_bfloat16* act;     // rows that go by
@@ -136,13 +151,14 @@ struct StreamArgs {
   const float* vec;             // vectors of the outer products, [..][rank]; null: none
   int vec_by_place;             // by place in the order, else by row
   const float* scales;          // of the vectors; null: 1
-  float *out, *part;            // [adapters][dim][rank] or (rank_major) [rank][dim]; chunks of adapters with several
+  float *out, *part;            // [adapters][dim][rank] or (rank_major) [rank][dim]; shares of segments that several runs have
   int rank_major;
   const int32_t *off, *perm;    // perm null: places are rows
   int* check_word;
-  int n, G, rank, chunk_rows, places;
+  int n, G, rank, runs;
+  int early;                    // all inputs but the vectors are older than the kernel in front, which waited before its trigger
 };
-cudaError_t launch_lowrank_stream(const StreamArgs& a, int chunks, cudaStream_t st);
+cudaError_t launch_lowrank_stream(const StreamArgs& a, cudaStream_t st);
 
 struct SumArgs {
   const float* planes;
@@ -164,8 +180,9 @@ struct UpArgs {
   size_t stride;
   int dim;
   const int32_t *off, *perm;
-  int n, G, segments, rank, chunk_rows, skip_none;
+  int n, G, segments, rank, runs, skip_none;
 };
-cudaError_t launch_lowrank_up(const UpArgs& a, int chunks, cudaStream_t st);
+// directly behind launch_lowrank_sum: all inputs but the vectors are older than that kernel
+cudaError_t launch_lowrank_up(const UpArgs& a, cudaStream_t st);
 
 }  // namespace emoe
