@@ -764,11 +764,12 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
     p.dim = a.out_dim;
     p.off = a.off;
     p.perm = a.perm;
+    p.check_word = a.check_word;
     p.n = a.n;
     p.G = a.G;
     p.segments = a.segments;
     p.rank = a.rank;
-    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, UP_CHANNELS), (a.rank <= 32 ? 2 : 1) * GPU_SMS, UP_ROWS, UP_RUN);
+    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, UP_RUN);
     p.skip_none = a.skip_none;
     e = launch_lowrank_up(p, st);
     if (e != cudaSuccess) return e;

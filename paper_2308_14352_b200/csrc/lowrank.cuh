@@ -135,11 +135,10 @@ __device__ __forceinline__ int share_of(const TileList& list, const TileRun& run
 
 // ---- many bf16 rows (lowrank_stream.cu) --------------------------------------------------------
 
-constexpr int UP_CHANNELS = 64 * LR_WARPS;  // channels of a CTA of the up kernel
-// ... of the stream kernel: as many as tensor memory has room for, beside the low-rank vectors
+// channels of a CTA: as many as tensor memory has room for
 __host__ __device__ constexpr int stream_channels(int rank) { return rank <= 32 ? 512 : 256; }
 constexpr int STREAM_ROWS = 128, STREAM_RUN = 8;  // rows of its tiles; tiles of its longest run: how many products are added in tensor memory
-constexpr int UP_ROWS = 64, UP_RUN = 32;
+constexpr int UP_RUN = 16;                          // tiles of the longest run of the up kernel
 
 struct StreamArgs {
   const __nv_bfloat16* act;     // rows that go by
@@ -180,6 +179,7 @@ struct UpArgs {
   size_t stride;
   int dim;
   const int32_t *off, *perm;
+  int* check_word;
   int n, G, segments, rank, runs, skip_none;
 };
 // directly behind launch_lowrank_sum: all inputs but the vectors are older than that kernel
