@@ -592,10 +592,11 @@ template <int H>
 __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
   __shared__ TileList list;
   const int tid = threadIdx.x, adapter = blockIdx.x, which = blockIdx.z;
+  // (the offsets are older than the kernel in front, which waited before its trigger)
+  const TileRun run = list_tiles<H>(list, a.off, a.G, a.n, 0, a.runs[which]);
   pdl_wait();
   pdl_trigger();
   if (!a.out[which]) return;
-  const TileRun run = list_tiles<H>(list, a.off, a.G, a.n, 0, a.runs[which]);
   const int first = list.first[adapter], end = list.first[adapter + 1], c0 = first / run.per, c1 = end > first ? (end - 1) / run.per : c0 - 1;
   if (c0 == c1) return;
   const size_t words = static_cast<size_t>(a.dim[which]) * a.rank / 4;  // dim is a multiple of 8

@@ -38,8 +38,9 @@ __device__ __forceinline__ void copy_arrive(uint32_t bar) { asm volatile("cp.asy
 
 // Copies the rows of a run, 128 channels at a time, into a ring of stages.  A thread copies 16 bytes of every eighth row of a tile; places
 // without a row and channels beyond the end become zeros (as does all that is not wanted).  FOR_MMA: the tensor cores read the
-// stage, so that the thread itself sees its copies land, fences them and arrives; it does so behind the wait for a free stage, which is no delay
-// since products leave a stage quickly.  Else threads read it, slowly, and the copies arrive by themselves.
+// stage, so that the thread itself sees its copies land, fences them and arrives, before it waits for the next free stage (behind that wait
+// the products of a stage would not start before those in front of it are done: 14 instead of 10 us per 67 MB).  Else threads read it
+// and the copies arrive by themselves.
 template <int STAGES, bool FOR_MMA>
 __device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted, size_t stride, int dim, int c0, int pairs, int tiles, const int* s_rows,
                                           uint32_t ring, uint32_t full, uint32_t empty, int thread, int* check_word, volatile int* abort_flag) {
@@ -62,18 +63,17 @@ __device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted,
     }
     for (int p = 0; p < pairs; ++p, ++it) {
       const int s = it % STAGES, c = c0 + p * 128 + piece * 8;
+      if constexpr (FOR_MMA) {
+        copy_wait<STAGES - 2>();
+        if (it >= STAGES - 1) landed(it - (STAGES - 1));
+      }
       ok = mbar_wait(empty + 8 * s, ((it / STAGES) & 1) ^ 1, check_word, abort_flag);
       if (!ok) break;
       const bool inside = c < dim;
 #pragma unroll
       for (int j = 0; j < STREAM_ROWS / 8; ++j) copy_async16(dst + s * STAGE + j * 1024, row[j] + (inside ? c : 0), inside && (live >> j & 1u));
-      if constexpr (FOR_MMA) {
-        copy_commit();
-        copy_wait<STAGES - 1>();
-        if (it >= STAGES - 1) landed(it - (STAGES - 1));
-      } else {
-        copy_arrive(full + 8 * s);
-      }
+      if constexpr (FOR_MMA) copy_commit();
+      else copy_arrive(full + 8 * s);
     }
   }
   copy_commit();
