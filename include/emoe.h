@@ -274,7 +274,8 @@ typedef struct emoe_lowrank_desc {
 } emoe_lowrank_desc;
 
 /* Context workspace that calls of at most n rows need (0 for an invalid description): pass the maximum over what the context
- * serves to emoe_create.  Forward calls of at most 512 rows, and fp32 ones with `off`, use none. */
+ * serves to emoe_create.  Forward calls of at most 1024 rows whose tensors are not large,
+ * and fp32 ones with `off`, use none. */
 size_t emoe_lowrank_workspace_bytes(const emoe_lowrank_desc* desc, int n);
 
 /* A [n_adapters][rank][in_dim], B [n_adapters][out_dim][rank]; scales NULL (1) or [n_adapters] fp32; x [n][in_dim]; y [n][out_dim];

@@ -229,13 +229,13 @@ __global__ void __launch_bounds__(SORT_THREADS)
   }
   if (bad) atomicOr(check_word, CHECK_BAD_EXPERT_ID);
   __syncthreads();
+  int of_warp[SORT_WARPS];  // of expert tid
   if (tid < E) {
     int sum = 0;
-    for (int w = 0; w < SORT_WARPS; ++w) {
-      const int c = first[w * E + tid];
-      first[w * E + tid] = sum;
-      sum += c;
-    }
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) of_warp[w] = first[w * E + tid];
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) sum += of_warp[w];
     hist[tid] = sum;
   }
   cluster.sync();
@@ -267,8 +267,12 @@ __global__ void __launch_bounds__(SORT_THREADS)
   }
   __syncthreads();
   if (tid < E) {
-    const int base = s_off[tid] + before;
-    for (int w = 0; w < SORT_WARPS; ++w) first[w * E + tid] += base;
+    int next = s_off[tid] + before;
+#pragma unroll
+    for (int w = 0; w < SORT_WARPS; ++w) {
+      first[w * E + tid] = next;
+      next += of_warp[w];
+    }
   }
   if (rank == 0)
     for (int e = tid; e <= E; e += SORT_THREADS) off[e] = s_off[e];

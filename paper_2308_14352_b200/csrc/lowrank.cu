@@ -14,6 +14,7 @@
 // low-rank vector of a bf16 result, whose own rounding is 2^-9.  Of the nine products of two values in three parts the three smallest
 // (2^-24 of the product) are left out.
 #include <cooperative_groups.h>
+#include <cstdlib>
 
 #include "lowrank.cuh"
 
@@ -22,7 +23,7 @@ namespace cg = cooperative_groups;
 namespace emoe {
 namespace {
 
-constexpr int LR_IDS_ROWS = 512;  // most rows whose adapters every CTA looks up by itself
+constexpr int LR_IDS_ROWS = 1024;  // most rows whose adapters every CTA looks up by itself
 
 struct LowrankArgs {
   const void *x, *base;  // rows in, rows added to the result (null: zeros)
@@ -37,63 +38,35 @@ struct LowrankArgs {
   size_t x_stride, y_stride;
 };
 
-// Which rows this cluster works on: their number and adapter (-1: none) or 0.  Rows are listed in shared memory.
-// ids: the first row of every BT rows with the same adapter leads them; off: tiles of BT rows, segment by segment.
+// Which rows this cluster works on: their number and adapter (-1: none) or 0.  Rows are listed in shared memory.  Segments are cut into tiles
+// of BT rows, one behind the other.  ids: every CTA counts the rows of each adapter, then lists those of its tile.
 template <int BT>
-__device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_rows, int* s_scan, int* adapter) {
+__device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_rows, int* s_scan, int* s_count, int* adapter) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int IDS = LR_IDS_ROWS / LR_THREADS;
+  int id[IDS];
   if (a.ids) {
-    int own = a.ids[tile];
-    if (own < 0 || own >= a.G) {
-      if (own != -1 && tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
-      own = -1;
-    }
-    *adapter = own;
-    unsigned same[LR_IDS_ROWS / LR_THREADS];
-    int before = 0;
 #pragma unroll
-    for (int i = 0; i < LR_IDS_ROWS / LR_THREADS; ++i) {
+    for (int i = 0; i < IDS; ++i) {
       const int j = i * LR_THREADS + tid;
-      int id = -2;
-      if (j < a.n) {
-        id = a.ids[j];
-        if (id < 0 || id >= a.G) id = -1;
+      id[i] = j < a.n ? a.ids[j] : -2;
+      if (j < a.n && (id[i] < 0 || id[i] >= a.G)) {
+        if (id[i] != -1 && tile == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
+        id[i] = a.G;
       }
-      same[i] = __ballot_sync(0xffffffffu, id == own);
-      const int chunk = i * LR_THREADS + warp * 32;  // first row of the ballot
-      if (lane == 0) s_scan[chunk / 32] = __popc(same[i]);
     }
+    for (int e = tid; e <= a.G; e += LR_THREADS) s_count[e] = 0;
     __syncthreads();
-    // rows with this adapter in front of the tile's own row, and in front of each chunk
-    for (int c = 0; c < tile / 32; ++c) before += s_scan[c];
-    int count = 0;
 #pragma unroll
-    for (int i = 0; i < LR_IDS_ROWS / LR_THREADS; ++i) {
-      const int chunk = i * (LR_THREADS / 32) + warp;
-      int front = 0;
-      for (int c = 0; c < chunk; ++c) front += s_scan[c];
-      if (chunk == tile / 32 && lane == 0) s_scan[LR_IDS_ROWS / 32] = before + __popc(same[i] & ((1u << (tile % 32)) - 1u));
-      same[i] = (same[i] >> lane & 1u) ? front + __popc(same[i] & ((1u << lane) - 1u)) : 0xffffffffu;  // now: rank, or none
-    }
+    for (int i = 0; i < IDS; ++i)
+      if (id[i] >= 0) atomicAdd(&s_count[id[i]], 1);
     __syncthreads();
-    const int first = s_scan[LR_IDS_ROWS / 32];
-    if (first % BT != 0) return 0;  // led by an earlier row
-    int total = 0;
-    for (int c = 0; c < LR_IDS_ROWS / 32; ++c) total += s_scan[c];
-    count = min(BT, total - first);
-#pragma unroll
-    for (int i = 0; i < LR_IDS_ROWS / LR_THREADS; ++i) {
-      const int rank = static_cast<int>(same[i]);
-      if (rank >= first && rank < first + BT) s_rows[rank - first] = i * LR_THREADS + tid;
-    }
-    __syncthreads();
-    return count;
   }
   // one thread per segment: its tiles, added up
   int begin = 0, rows = 0;
   if (tid < a.segments) {
-    begin = min(max(a.off[tid], 0), a.n);
-    rows = min(a.off[tid + 1], a.n) - begin;
+    begin = a.ids ? 0 : min(max(a.off[tid], 0), a.n);
+    rows = a.ids ? s_count[tid] : min(a.off[tid + 1], a.n) - begin;
   }
   const int tiles = rows > 0 ? (rows + BT - 1) / BT : 0;
   int incl = tiles;
@@ -105,8 +78,11 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
   if (lane == 31) s_scan[warp] = incl;
   if (tid == 0) s_scan[LR_WARPS] = 0;
   // (a 257th segment, the rows of no adapter beside 256 of them)
-  const int last_begin = a.segments > LR_THREADS ? min(max(a.off[LR_THREADS], 0), a.n) : 0;
-  const int last_rows = a.segments > LR_THREADS ? min(a.off[LR_THREADS + 1], a.n) - last_begin : 0;
+  int last_begin = 0, last_rows = 0;
+  if (a.segments > LR_THREADS) {
+    last_begin = a.ids ? 0 : min(max(a.off[LR_THREADS], 0), a.n);
+    last_rows = a.ids ? s_count[LR_THREADS] : min(a.off[LR_THREADS + 1], a.n) - last_begin;
+  }
   __syncthreads();
   int front = 0, all = 0;
   for (int w = 0; w < LR_WARPS; ++w) {
@@ -128,7 +104,26 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
   const int count = s_scan[LR_WARPS], at = s_scan[LR_WARPS + 1], g = s_scan[LR_WARPS + 2];
   if (count == 0) return 0;
   *adapter = g < a.G ? g : -1;
-  for (int i = tid; i < count; i += LR_THREADS) s_rows[i] = a.perm ? a.perm[at + i] : at + i;
+  if (!a.ids) {
+    for (int i = tid; i < count; i += LR_THREADS) s_rows[i] = a.perm ? a.perm[at + i] : at + i;
+    __syncthreads();
+    return count;
+  }
+  // places at .. at + count - 1 among the rows of the adapter, which a warp's ballots and the counts in front of it give
+  unsigned same[IDS];
+#pragma unroll
+  for (int i = 0; i < IDS; ++i) {
+    same[i] = __ballot_sync(0xffffffffu, id[i] == g);
+    if (lane == 0) s_count[i * LR_WARPS + warp] = __popc(same[i]);  // (every thread has its counts: they are read in front of the last barrier)
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < IDS; ++i) {
+    if (id[i] != g) continue;
+    int place = __popc(same[i] & ((1u << lane) - 1u));
+    for (int c = 0; c < i * LR_WARPS + warp; ++c) place += s_count[c];
+    if (place >= at && place < at + count) s_rows[place - at] = i * LR_THREADS + tid;
+  }
   __syncthreads();
   return count;
 }
@@ -182,21 +177,22 @@ struct Lowrank {
 };
 
 template <typename T, int RT, int NT, bool BACK>
-__global__ void __launch_bounds__(LR_THREADS, RT * NT <= 8 && sizeof(T) == 2 ? 2 : 1) lowrank_kernel(LowrankArgs a) {
+__global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ? 2 : 1) ? 2 : 1) lowrank_kernel(LowrankArgs a) {
   using L = Lowrank<T, RT, NT, BACK>;
   constexpr int BT = L::BT, RP = L::RP, PI = L::PI, PV = L::PV, WORDS = L::WORDS, KS = L::KS;
   extern __shared__ __align__(16) char smem[];
   float* s_red = reinterpret_cast<float*>(smem);
   float* s_part = s_red + L::RED_FLOATS;
   __nv_bfloat16* s_v = reinterpret_cast<__nv_bfloat16*>(s_part + L::PART_FLOATS);
-  __shared__ int s_rows[BT], s_scan[LR_IDS_ROWS / 32 + 1];
+  __shared__ int s_rows[BT], s_scan[LR_WARPS + 3], s_count[EMOE_MAX_EXPERTS + 1];
+  static_assert(LR_IDS_ROWS / 32 <= EMOE_MAX_EXPERTS, "the warps' counts lie where the adapters' were");
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q = lane & 3;
   const int ctas = static_cast<int>(cluster.num_blocks()), cta = static_cast<int>(cluster.block_rank());
   pdl_wait();
   pdl_trigger();
   int adapter = -1;
-  const int count = find_rows<BT>(a, blockIdx.x / ctas, s_rows, s_scan, &adapter);
+  const int count = find_rows<BT>(a, blockIdx.x / ctas, s_rows, s_scan, s_count, &adapter);
   if (count == 0 || (adapter < 0 && a.skip_none && !a.v)) return;  // the whole cluster
   const T* down = static_cast<const T*>(a.down) + static_cast<size_t>(adapter < 0 ? 0 : adapter) * a.rank * a.in_dim;
   const T* up = static_cast<const T*>(a.up) + static_cast<size_t>(adapter < 0 ? 0 : adapter) * a.rank * a.out_dim;
@@ -615,8 +611,6 @@ __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
 
 // ---- launches -----------------------------------------------------------------------------------
 
-// Rows from which bf16 calls take the streaming kernels.
-constexpr int LR_STREAM_ROWS = 512;
 
 struct LowrankLayout {
   size_t off, perm, vec, planes, part[2], total;  // vec: dv, or the vectors in the order; planes: their shares
@@ -631,7 +625,14 @@ int runs_for(int n, int segments, int blocks, int slots, int tile, int most) {
   const int least = (tiles + most - 1) / most, runs = (least + side - 1) / side * side;
   return runs < tiles ? runs : tiles;
 }
-bool takes_stream(const emoe_lowrank_desc& D, int n) { return D.dtype == EMOE_DTYPE_BF16 && n > LR_STREAM_ROWS; }
+// Which bf16 calls take the streaming kernels, by the bytes of the rows in, added and out: those three (and their launches) cost some 10 us
+// more at the start and run at the speed of memory from there on.  us, fused / streaming, 4096 -> 4096: rank 16, 2048 rows 15.9/20.6, 3072 rows 25/26;
+// rank 64, 1024 rows 25/35, 1536 rows 35/32, 3072 rows 57/39; rank 16, 1024 -> 1024, 3072 rows 8.4/14.5.
+bool takes_stream(const emoe_lowrank_desc& D, int n) {
+  const double bytes = 2.0 * n * (static_cast<double>(D.in_dim) + 2.0 * D.out_dim);
+  if (getenv("SR")) return D.dtype == EMOE_DTYPE_BF16 && n > atoi(getenv("SR"));
+  return D.dtype == EMOE_DTYPE_BF16 && bytes > (D.rank > 32 ? 32e6 : 80e6);
+}
 
 LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
   const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
@@ -684,19 +685,21 @@ cudaError_t launch_tile(const LowrankArgs& a, int tiles, int ctas, cudaStream_t 
 
 template <typename T, bool BACK>
 cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
-  // Rows per tile by the mean rows of an adapter; CTAs per tile until the tiles fill the GPU twice.
-  const int groups = a.n < a.G ? a.n : a.G, mean = (a.n + groups - 1) / groups;
-  const int nt = mean <= 8 ? 1 : mean <= 48 || (sizeof(T) == 4 && a.rank > 32) ? 4 : 8;
-  const int full = (a.n + nt * 8 - 1) / (nt * 8), tiles = a.ids ? a.n : full + (a.segments < a.n ? a.segments : a.n);
-  const int busy = full > groups ? full : groups;
+  // Rows per tile: 8, which has the most CTAs to share the work, while those are few; then 32, which read the factors a quarter as often.
+  // us, 4096 -> 4096, rank 16, 8 / 32 rows: bf16 512 rows 10.2/10.6, 1024 rows 17.5/15.1, 2048 rows 26/16; fp32 515 rows of 1104 -> 776 8.8/11.0, 2048 rows
+  // 58/40.  At a rank beyond 32 the registers of the larger tile leave an SM one CTA: 1024 rows 25/36 (bf16), 44/47 (fp32, 2048 -> 2048).
+  // 64 rows were slower or as fast everywhere (2048 rows 20 us).
+  const int segments = a.segments < a.n ? a.segments : a.n;
+  const auto mean_tiles = [&](int rows) { return a.n / rows + (segments + 1) / 2; };
+  const int nt = mean_tiles(8) <= (a.rank > 32 ? 264 : 104) ? 1 : 4;
+  // CTAs per tile while all of them run side by side: two per SM, or one where 32 rows take the registers of both
+  const int slots = nt == 4 && a.rank > (sizeof(T) == 2 ? 32 : 16) ? GPU_SMS : 2 * GPU_SMS;
   int ctas = 1;
-  while (ctas < 8 && busy * ctas * 2 <= 2 * GPU_SMS) ctas *= 2;
+  while (ctas < 8 && mean_tiles(nt * 8) * ctas * 2 <= slots) ctas *= 2;
+  const int tiles = a.n / (nt * 8) + segments;
   const auto by_rows = [&](auto rt) -> cudaError_t {
     constexpr int RT = decltype(rt)::value;
-    if (nt == 1) return launch_tile<T, RT, 1, BACK>(a, tiles, ctas, st);
-    if (nt == 4) return launch_tile<T, RT, 4, BACK>(a, tiles, ctas, st);
-    if constexpr (sizeof(T) == 2 || RT < 4) return launch_tile<T, RT, 8, BACK>(a, tiles, ctas, st);
-    return cudaErrorInvalidValue;  // not reached: nt is 4 there
+    return nt == 1 ? launch_tile<T, RT, 1, BACK>(a, tiles, ctas, st) : launch_tile<T, RT, 4, BACK>(a, tiles, ctas, st);
   };
   if (a.rank <= 16) return by_rows(std::integral_constant<int, 1>());
   if (a.rank <= 32) return by_rows(std::integral_constant<int, 2>());
@@ -852,8 +855,9 @@ int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const voi
   size_t have = 0;
   char* ws = ctx_workspace(ctx, &have);
   const LowrankLayout w = lowrank_layout(*desc, n);
-  if (ids && n <= LR_IDS_ROWS) {
+  if (ids && n <= LR_IDS_ROWS && !takes_stream(*desc, n)) {
     a.ids = ids;
+    a.segments = desc->n_adapters + 1;
   } else if (off && takes_stream(*desc, n)) {
     if (w.part[0] > have) return EMOE_ERR_WORKSPACE;
   } else if (ids) {

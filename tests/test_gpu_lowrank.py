@@ -144,8 +144,11 @@ CASES = [
     (200, 136, 96, 2, 33, F32, {"none": 0.5}),
     (130, 256, 512, 1, 64, BF16, {}),
     (130, 256, 512, 1, 64, F32, {}),
-    (512, 264, 136, 7, 24, BF16, {"skew": 1.1}),                       # the last size whose rows every CTA looks up
-    (513, 264, 136, 7, 24, BF16, {"skew": 1.1, "none": 0.1}),          # the first that is sorted
+    (512, 264, 136, 7, 24, BF16, {"skew": 1.1}),
+    (513, 264, 136, 7, 24, BF16, {"skew": 1.1, "none": 0.1}),
+    (1024, 264, 136, 7, 24, BF16, {"skew": 1.1}),                      # the last size whose rows every CTA looks up
+    (1025, 264, 136, 7, 24, BF16, {"skew": 1.1, "none": 0.1}),         # the first that is sorted
+    (1024, 136, 64, 256, 16, F32, {"none": 0.3}),
     (777, 72, 2056, 256, 4, BF16, {"none": 0.3}),                      # all adapters there can be, and rows of none
     (1500, 200, 88, 256, 16, F32, {}),
     (2100, 512, 512, 3, 32, BF16, {"skew": 2.0}),
@@ -156,6 +159,17 @@ CASES = [
     (40, 384, 640, 8, 32, BF16, {"kind": "off", "none": 0.25}),
     (3000, 1024, 1032, 4, 16, BF16, {"kind": "off", "skew": 1.5}),     # several chunks of rows per adapter, and adapters with one
     (5, 128, 128, 200, 16, BF16, {"kind": "off"}),                     # most adapters without rows
+    # bytes of the rows enough for the streaming kernels
+    (4000, 2056, 4104, 5, 16, BF16, {"skew": 1.0}),                    # channels that end inside a tile, one value of them
+    (4001, 2056, 4104, 256, 12, BF16, {"none": 0.4}),                  # short segments, several to a tile's rows, and a long one of none
+    (2500, 4104, 6152, 3, 5, BF16, {"pad": (8, 24)}),                  # odd rank: vectors and factors by single values
+    (9000, 1032, 2048, 1, 32, BF16, {}),                               # one adapter: every run is part of its rows
+    (5000, 2048, 3080, 100, 20, BF16, {"kind": "off", "skew": 1.5, "none": 0.2}),
+    (1300, 4096, 8200, 2, 64, BF16, {"kind": "off"}),
+    (3000, 2056, 2056, 9, 40, BF16, {"none": 0.1, "skew": 2.0}),
+    (2200, 2048, 3000, 200, 33, BF16, {}),
+    (40000, 520, 264, 3, 16, BF16, {"skew": 1.0}),                     # more tiles than one round of runs holds
+    (20000, 72, 520, 30, 64, BF16, {"kind": "off", "none": 0.01}),
 ]
 
 
@@ -333,15 +347,16 @@ def test_gradients_against_differences(ctx):
 
 
 def test_workspace_is_checked(ctx):
-    c = Case(600, 64, 64, 4, 8, BF16)
-    need = B.emoe_lowrank_workspace_bytes(c.desc, 600)
-    assert need > 0 and B.emoe_lowrank_workspace_bytes(c.desc, 601) >= need
+    n = 1100                                       # (forward calls of up to 1024 rows need none)
+    c = Case(n, 64, 64, 4, 8, BF16)
+    need = B.emoe_lowrank_workspace_bytes(c.desc, n)
+    assert need > 0 and B.emoe_lowrank_workspace_bytes(c.desc, n + 1) >= need
     small = B.emoe_create(0, 1024)
     with pytest.raises(B.EmoeError) as e:
         c.forward(small)
     assert e.value.status == B.ERR_WORKSPACE
     with pytest.raises(B.EmoeError) as e:
-        c.backward(small, torch.zeros(600, 8, device="cuda"))
+        c.backward(small, torch.zeros(n, 8, device="cuda"))
     assert e.value.status == B.ERR_WORKSPACE
     B.emoe_destroy(small)
     exact = B.emoe_create(0, need)
