@@ -14,7 +14,6 @@
 // low-rank vector of a bf16 result, whose own rounding is 2^-9.  Of the nine products of two values in three parts the three smallest
 // (2^-24 of the product) are left out.
 #include <cooperative_groups.h>
-#include <cstdlib>
 
 #include "lowrank.cuh"
 
@@ -299,7 +298,16 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
             }
           }
 #pragma unroll
-          for (int m = 0; m < RT; ++m) mma_parts<PI, PI>(acc[m][t], af[m], bf);
+          for (int m = 0; m < RT; ++m) {
+            if constexpr (PI == 1) {
+              mma_parts<PI, PI>(acc[m][t], af[m], bf);
+            } else {  // the tensor cores cut what they add: sixteen products of fp32 values are summed by themselves, then added with rounding
+              float d[4] = {};
+              mma_parts<PI, PI>(d, af[m], bf);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[m][t][i] += d[i];
+            }
+          }
         }
       }
     }
@@ -625,18 +633,18 @@ int runs_for(int n, int segments, int blocks, int slots, int tile, int most) {
   const int least = (tiles + most - 1) / most, runs = (least + side - 1) / side * side;
   return runs < tiles ? runs : tiles;
 }
-// Which bf16 calls take the streaming kernels, by the bytes of the rows in, added and out: those three (and their launches) cost some 10 us
-// more at the start and run at the speed of memory from there on.  us, fused / streaming, 4096 -> 4096: rank 16, 2048 rows 15.9/20.6, 3072 rows 25/26;
-// rank 64, 1024 rows 25/35, 1536 rows 35/32, 3072 rows 57/39; rank 16, 1024 -> 1024, 3072 rows 8.4/14.5.
-bool takes_stream(const emoe_lowrank_desc& D, int n) {
-  const double bytes = 2.0 * n * (static_cast<double>(D.in_dim) + 2.0 * D.out_dim);
-  if (getenv("SR")) return D.dtype == EMOE_DTYPE_BF16 && n > atoi(getenv("SR"));
-  return D.dtype == EMOE_DTYPE_BF16 && bytes > (D.rank > 32 ? 32e6 : 80e6);
+// Which bf16 calls take the streaming kernels, by the bytes of the rows read and written: they (and their launches) cost some 10 us more at the
+// start and run at the speed of memory from there on.  us, fused / streaming, 4096 -> 4096.  Forward, rank 16: 2048 rows 15.9/20.6, 3072 rows
+// 25/26; rank 64: 1024 rows 25/35, 1536 rows 35/32.  Backward, rank 16: 512 rows 29.6/30.5, 1024 rows 41/29 (1024 -> 1024: 2048 rows 21/24, 4096 rows
+// 31/28); rank 64: 256 rows 59/63, 512 rows 75/66.
+bool takes_stream(const emoe_lowrank_desc& D, int n, bool back) {
+  const double K = D.in_dim, N = D.out_dim, bytes = 2.0 * n * (back ? 3 * K + N : K + 2 * N);
+  return D.dtype == EMOE_DTYPE_BF16 && bytes > (back ? (D.rank > 32 ? 12e6 : 20e6) : (D.rank > 32 ? 32e6 : 80e6));
 }
 
-LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
+LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n, bool back) {
   const auto up = [](size_t v) { return (v + 255) / 256 * 256; };
-  const bool stream = takes_stream(D, n);
+  const bool stream = takes_stream(D, n, back);
   LowrankLayout w{};
   const size_t vectors = sizeof(float) * static_cast<size_t>(n) * D.rank;
   size_t o = 0;
@@ -647,14 +655,15 @@ LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n) {
   if (stream) o += up(vectors * blocks_of(D.in_dim > D.out_dim ? D.in_dim : D.out_dim, stream_channels(D.rank)));
   for (int i = 0; i < 2; ++i) {
     const size_t dim = i ? D.in_dim : D.out_dim;
+    w.part[i] = o;
+    if (!back) continue;
     // 1024 rows at most per run, as accuracy goes on the streaming path
     w.runs[i] = runs_for(n, D.n_adapters, blocks_of(static_cast<int>(dim), stream ? stream_channels(D.rank) : GR_CHANNELS), GPU_SMS,
-                         stream ? STREAM_ROWS : GR_ROWS, stream ? STREAM_RUN : STREAM_RUN * STREAM_ROWS / GR_ROWS);
-    w.part[i] = o;
+                         stream ? GRANULE : GR_ROWS, stream ? STREAM_RUN : STREAM_RUN * GRANULE / GR_ROWS);
     // Two shares per run.  What is reserved grows with n, dim and rank alike, so that a context that is made for the largest call serves all:
-    // runs <= slots / blocks + tiles / 8 + 1 and slots / blocks * dim <= slots * 512; runs <= tiles.
-    const size_t tiles = (static_cast<size_t>(n) + 63) / 64 + (D.n_adapters < n ? D.n_adapters : n);
-    const size_t even = static_cast<size_t>(2 * GPU_SMS) * 512 + (tiles / 8 + 2) * dim;
+    // runs <= slots / blocks + granules / 64 + 1 and slots / blocks * dim <= slots * 512; runs <= granules.
+    const size_t tiles = (static_cast<size_t>(n) + GRANULE - 1) / GRANULE + (D.n_adapters < n ? D.n_adapters : n);
+    const size_t even = static_cast<size_t>(2 * GPU_SMS) * 512 + (tiles / STREAM_RUN + 2) * dim;
     o += up(sizeof(float) * 2 * (tiles * dim < even ? tiles * dim : even) * D.rank);
   }
   w.total = o;
@@ -709,7 +718,7 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
 cudaError_t launch_join(const GradArgs& a, bool stream, cudaStream_t st) {
   const size_t dim = a.dim[0] > a.dim[1] ? a.dim[0] : a.dim[1], shares = (dim * a.rank / 4 + LR_THREADS - 1) / LR_THREADS;
   const dim3 grid(a.G, static_cast<unsigned>(shares < 32 ? shares : 32), 2);
-  if (stream) return launch_chain(lowrank_join_kernel<STREAM_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
+  if (stream) return launch_chain(lowrank_join_kernel<GRANULE>, grid, dim3(LR_THREADS), 0, st, a);
   return launch_chain(lowrank_join_kernel<GR_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
 }
 
@@ -748,7 +757,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
   s.n = a.n;
   s.G = a.G;
   s.rank = a.rank;
-  s.runs = runs_for(a.n, a.G, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, STREAM_RUN);
+  s.runs = runs_for(a.n, a.G, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, GRANULE, STREAM_RUN);
   if (back && ga->out[0]) outer(0, &s);
   cudaError_t e = cudaSuccess;
   if (s.factor || s.vec) e = launch_lowrank_stream(s, st);
@@ -773,7 +782,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
     p.G = a.G;
     p.segments = a.segments;
     p.rank = a.rank;
-    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, UP_RUN);
+    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, stream_channels(a.rank)), GPU_SMS, GRANULE, UP_RUN);
     p.skip_none = a.skip_none;
     e = launch_lowrank_up(p, st);
     if (e != cudaSuccess) return e;
@@ -819,7 +828,8 @@ extern "C" {
 size_t emoe_lowrank_workspace_bytes(const emoe_lowrank_desc* desc, int n) {
   int32_t given = 0;
   if (check_lowrank(desc, n, &given, nullptr) != EMOE_OK) return 0;
-  return lowrank_layout(*desc, n).total;  // grows with n
+  const size_t forward = lowrank_layout(*desc, n, false).total, backward = lowrank_layout(*desc, n, true).total;
+  return forward > backward ? forward : backward;
 }
 
 int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const void* A, const void* B, const float* scales, const void* x, int n,
@@ -854,21 +864,22 @@ int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const voi
   a.off = off;
   size_t have = 0;
   char* ws = ctx_workspace(ctx, &have);
-  const LowrankLayout w = lowrank_layout(*desc, n);
-  if (ids && n <= LR_IDS_ROWS && !takes_stream(*desc, n)) {
+  const LowrankLayout w = lowrank_layout(*desc, n, false);
+  const bool streams = takes_stream(*desc, n, false);
+  if (ids && n <= LR_IDS_ROWS && !streams) {
     a.ids = ids;
     a.segments = desc->n_adapters + 1;
-  } else if (off && takes_stream(*desc, n)) {
-    if (w.part[0] > have) return EMOE_ERR_WORKSPACE;
+  } else if (off && streams) {
+    if (w.total > have) return EMOE_ERR_WORKSPACE;
   } else if (ids) {
-    if ((takes_stream(*desc, n) ? w.part[0] : w.vec) > have) return EMOE_ERR_WORKSPACE;
+    if ((streams ? w.total : w.vec) > have) return EMOE_ERR_WORKSPACE;
     int32_t *off_ws = reinterpret_cast<int32_t*>(ws + w.off), *perm = reinterpret_cast<int32_t*>(ws + w.perm);
     EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, nullptr, a.check_word, st));
     a.off = off_ws;
     a.perm = perm;
     a.segments = desc->n_adapters + 1;
   }
-  if (takes_stream(*desc, n)) EMOE_CALL(ctx, launch_many(a, false, nullptr, ws, w, st));
+  if (streams) EMOE_CALL(ctx, launch_many(a, false, nullptr, ws, w, st));
   else EMOE_CALL(ctx, desc->dtype == EMOE_DTYPE_BF16 ? (launch_lowrank<__nv_bfloat16, false>(a, st)) : (launch_lowrank<float, false>(a, st)));
   return EMOE_OK;
 }
@@ -886,7 +897,8 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   if (!ctx) return EMOE_ERR_INVALID_ARG;
   size_t have = 0;
   char* ws = ctx_workspace(ctx, &have);
-  const LowrankLayout w = lowrank_layout(*desc, n);
+  const LowrankLayout w = lowrank_layout(*desc, n, true);
+  const bool streams = takes_stream(*desc, n, true);
   if (w.total > have) return EMOE_ERR_WORKSPACE;
   const CallScope scope(ctx);
   EMOE_CALL(ctx, scope.error());
@@ -900,7 +912,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   a.up = A;
   a.scales = scales;
   a.y = dx;
-  a.v = dA && !takes_stream(*desc, n) ? dv : nullptr;
+  a.v = dA && !streams ? dv : nullptr;
   a.check_word = ctx_check_word(ctx);
   a.n = n;
   a.G = a.segments = desc->n_adapters;
@@ -939,14 +951,14 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
     ga.blocks[i] = ga.out[i] ? (ga.dim[i] + GR_CHANNELS - 1) / GR_CHANNELS : 0;
     ga.runs[i] = w.runs[i];
   }
-  if (takes_stream(*desc, n)) {
+  if (streams) {
     EMOE_CALL(ctx, launch_many(a, true, &ga, ws, w, st));
   } else {
     const bool bf16 = desc->dtype == EMOE_DTYPE_BF16;
     if (dx || dA) EMOE_CALL(ctx, bf16 ? (launch_lowrank<__nv_bfloat16, true>(a, st)) : (launch_lowrank<float, true>(a, st)));
     if (dA || dB) EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, st) : launch_grads<float>(ga, st));
   }
-  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, takes_stream(*desc, n), st));
+  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, streams, st));
   return EMOE_OK;
 }
 

@@ -137,8 +137,31 @@ __device__ __forceinline__ int share_of(const TileList& list, const TileRun& run
 
 // channels of a CTA: as many as tensor memory has room for
 __host__ __device__ constexpr int stream_channels(int rank) { return rank <= 32 ? 512 : 256; }
-constexpr int STREAM_ROWS = 128, STREAM_RUN = 8;  // rows of its tiles; tiles of its longest run: how many products are added in tensor memory
-constexpr int UP_RUN = 16;                          // tiles of the longest run of the up kernel
+constexpr int STREAM_ROWS = 128;  // rows of their tiles at most
+// The kernels' runs are counted in granules of 16 rows, so that they are even in rows, not in tiles of which some are short; a CTA cuts
+// its own run into tiles.  Granules of the longest run: how many products are added in tensor memory; how many rows a CTA lists.
+constexpr int GRANULE = 16, STREAM_RUN = 64, UP_RUN = 128;
+struct RunTile {
+  int begin, rows;    // in the order
+  int list;           // of its first row in the CTA's list of rows
+  bool starts, ends;  // the first, the last of its segment within the run
+};
+struct RunWalk {
+  const TileList& list;
+  TileRun run;
+  int at, segment;
+  __device__ __forceinline__ RunWalk(const TileList& l, const TileRun& r) : list(l), run(r), at(r.lo), segment(l.segment) {}
+  __device__ __forceinline__ bool more() const { return at < run.hi; }
+  __device__ __forceinline__ RunTile next() {
+    while (at >= list.first[segment + 1]) ++segment;
+    const int first = list.first[segment], end = min(run.hi, list.first[segment + 1]), take = min(STREAM_ROWS / GRANULE, end - at);
+    const int in_segment = (at - first) * GRANULE;
+    const RunTile t = {list.begin[segment] + in_segment, min(take * GRANULE, list.rows[segment] - in_segment), (at - run.lo) * GRANULE,
+                       at == run.lo || at == first, at + take == end};
+    at += take;
+    return t;
+  }
+};
 
 struct StreamArgs {
   const __nv_bfloat16* act;     // rows that go by

@@ -42,7 +42,7 @@ __device__ __forceinline__ void copy_arrive(uint32_t bar) { asm volatile("cp.asy
 // the products of a stage would not start before those in front of it are done: 14 instead of 10 us per 67 MB).  Else threads read it
 // and the copies arrive by themselves.
 template <int STAGES, bool FOR_MMA>
-__device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted, size_t stride, int dim, int c0, int pairs, int tiles, const int* s_rows,
+__device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted, size_t stride, int dim, int c0, int pairs, RunWalk walk, const int* s_rows,
                                           uint32_t ring, uint32_t full, uint32_t empty, int thread, int* check_word, volatile int* abort_flag) {
   const int piece = thread & 15, row0 = thread >> 4;
   const uint32_t dst = ring + (piece >> 3) * TILE + row0 * 128 + (((piece & 7) ^ row0) << 4);
@@ -53,11 +53,12 @@ __device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted,
     fence_async_proxy();
     mbar_arrive(full + 8 * (stage % STAGES));
   };
-  for (int t = 0; t < tiles && ok; ++t) {
+  while (walk.more() && ok) {
+    const RunTile tile = walk.next();
     uint32_t live = 0;
 #pragma unroll
     for (int j = 0; j < STREAM_ROWS / 8; ++j) {
-      const int r = s_rows[t * STREAM_ROWS + row0 + 8 * j];
+      const int r = row0 + 8 * j < tile.rows ? s_rows[tile.list + row0 + 8 * j] : -1;
       if (r >= 0 && wanted) live |= 1u << j;
       row[j] = act + static_cast<size_t>(max(r, 0)) * stride;
     }
@@ -90,7 +91,7 @@ __device__ __forceinline__ void put_factor(char* tiles, const __nv_bfloat16* fac
     const uint16_t* f = reinterpret_cast<const uint16_t*>(factor) + (static_cast<size_t>(adapter) * dim + c0) * rank;
     constexpr int N = CHANNELS / SIDE;
     if (rank % 8 == 0) {
-#pragma unroll
+#pragma unroll 1
       for (int r0 = 0; r0 < RP; r0 += 16) {
         uint4 w[N][2];
 #pragma unroll
@@ -129,19 +130,26 @@ __device__ __forceinline__ void put_factor(char* tiles, const __nv_bfloat16* fac
   }
 }
 
-// RP values of a low-rank vector, zeros beyond its rank
-template <int RP>
-__device__ __forceinline__ void load_vector(const float* v, int rank, bool live, float (&f)[RP]) {
+// N values of a low-rank vector, zeros from `count` on; words: vectors are whole 16-byte words
+template <int N>
+__device__ __forceinline__ void load_vector(const float* v, int count, bool words, bool live, float (&f)[N]) {
 #pragma unroll
-  for (int r = 0; r < RP; r += 4) {
-    if (rank % 4 == 0) {
-      const float4 u = live && r < rank ? *reinterpret_cast<const float4*>(v + r) : make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int r = 0; r < N; r += 4) {
+    if (words) {
+      const float4 u = live && r < count ? *reinterpret_cast<const float4*>(v + r) : make_float4(0.f, 0.f, 0.f, 0.f);
       f[r] = u.x; f[r + 1] = u.y; f[r + 2] = u.z; f[r + 3] = u.w;
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) f[r + i] = live && r + i < rank ? v[r + i] : 0.f;
+      for (int i = 0; i < 4; ++i) f[r + i] = live && r + i < count ? v[r + i] : 0.f;
     }
   }
+}
+
+// the segment that follows in a run that has more
+__device__ __forceinline__ int list_next(const TileList& list, const RunWalk& walk) {
+  int s = walk.segment;
+  while (walk.at >= list.first[s + 1]) ++s;
+  return s;
 }
 
 constexpr uint32_t BF16_F32 = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);  // instruction descriptor: bf16 x bf16 -> fp32, M = 128
@@ -158,12 +166,14 @@ template <int RT>
 struct Stream {
   static constexpr int RP = RT * 16, CHANNELS = stream_channels(RP), PAIRS = CHANNELS / 128;
   static constexpr int FACTOR = CHANNELS / 64 * RP * 128;      // [rank][channels], K-major tiles of 64 channels
-  static constexpr int VEC = 2 * 3 * RP * 128;                 // [three parts of rank][128 rows], K-major tiles of 64 rows
-  static constexpr int VEC_BUFS = RT == 4 ? 1 : 2;
+  static constexpr int VEC = (3 * RP + 63) / 64 * TILE;        // [128 rows][three parts of rank], tiles of 64 values
+  __host__ __device__ static constexpr int vec_bufs(bool down) { return RT == 4 || (RT == 2 && down) ? 1 : 2; }
   static constexpr int COL_OUTER = 2 * RP, COLS = COL_OUTER + PAIRS * 3 * RP, TMEM = COLS <= 256 ? 256 : 512;
   static_assert(COLS <= 512, "tensor memory has 512 columns");
+  // two factors where there is room: the next segment's comes in ahead (a change of segments stops the products for some 3 us else)
+  __host__ __device__ static constexpr int factor_bufs(bool outer) { return RT == 1 || !outer ? 2 : 1; }
   static constexpr size_t smem(bool down, bool outer) {
-    return 1024 + static_cast<size_t>(SK_STAGES) * STAGE + (down ? FACTOR : 0) + (outer ? VEC_BUFS * VEC : 0) + sizeof(int) * STREAM_RUN * STREAM_ROWS + sizeof(TileList);
+    return 1024 + static_cast<size_t>(SK_STAGES) * STAGE + (down ? factor_bufs(outer) * FACTOR : 0) + (outer ? vec_bufs(down) * VEC : 0) + sizeof(int) * STREAM_RUN * GRANULE + sizeof(TileList);
   }
 };
 
@@ -176,19 +186,19 @@ struct Stream {
 template <int RT, bool DOWN, bool OUTER>
 __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArgs a) {
   using S = Stream<RT>;
-  constexpr int RP = S::RP, PAIRS = S::PAIRS;
+  constexpr int RP = S::RP, PAIRS = S::PAIRS, VEC_BUFS = S::vec_bufs(DOWN), FACTOR_BUFS = S::factor_bufs(OUTER);
   extern __shared__ char smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * SK_STAGES + 12];
+  __shared__ __align__(8) uint64_t bars[2 * SK_STAGES + 12];  // full, empty: stages; ready: factors
   __shared__ uint32_t tmem_slot;
   __shared__ int wait_words[PIPE_WORDS];
   volatile int* abort_flag = wait_words + PIPE_ABORT;
   char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   char* s_factor = smem + SK_STAGES * STAGE;
-  char* s_vec = s_factor + (DOWN ? S::FACTOR : 0);
-  int* s_rows = reinterpret_cast<int*>(s_vec + (OUTER ? S::VEC_BUFS * S::VEC : 0));
-  TileList& list = *reinterpret_cast<TileList*>(s_rows + STREAM_RUN * STREAM_ROWS);
+  char* s_vec = s_factor + (DOWN ? FACTOR_BUFS * S::FACTOR : 0);
+  int* s_rows = reinterpret_cast<int*>(s_vec + (OUTER ? VEC_BUFS * S::VEC : 0));
+  TileList& list = *reinterpret_cast<TileList*>(s_rows + STREAM_RUN * GRANULE);
   const uint32_t full = smem_u32(bars), empty = full + 8 * SK_STAGES, d1_full = empty + 8 * SK_STAGES, d1_empty = d1_full + 16,
-                 vec_full = d1_empty + 16, vec_empty = vec_full + 16, ready = vec_empty + 16, d2_full = ready + 8, d2_empty = d2_full + 8;
+                 vec_full = d1_empty + 16, vec_empty = vec_full + 16, ready = vec_empty + 16, d2_full = ready + 16, d2_empty = d2_full + 8;
   const int tid = threadIdx.x, warp = uniform_warp();
   if (tid == 0) {
     for (int i = 0; i < SK_STAGES; ++i) {
@@ -200,8 +210,8 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
       mbar_init(d1_empty + 8 * i, SIDE);
       mbar_init(vec_full + 8 * i, SIDE);
       mbar_init(vec_empty + 8 * i, 1);
+      mbar_init(ready + 8 * i, SIDE);
     }
-    mbar_init(ready, SIDE);
     mbar_init(d2_full, 1);
     mbar_init(d2_empty, SIDE);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -209,7 +219,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     wait_words[PIPE_FRONT] = a.early;
   }
   if (!a.early) pdl_wait();
-  const TileRun run = list_tiles<STREAM_ROWS>(list, a.off, a.G, a.n, blockIdx.x, a.runs);
+  const TileRun run = list_tiles<GRANULE>(list, a.off, a.G, a.n, blockIdx.x, a.runs);
   if (run.lo >= run.hi) {
     pdl_wait();
     pdl_trigger();
@@ -220,36 +230,36 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     if (tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
     return;
   }
-  for (int t = run.lo + warp, s = list.segment; t < run.hi; t += SK_THREADS / 32) {
-    const Tile tile = tile_of<STREAM_ROWS>(list, run, t, &s);
-    for (int i = tid & 31; i < STREAM_ROWS; i += 32)
-      s_rows[(t - run.lo) * STREAM_ROWS + i] = i < tile.rows ? (a.perm ? a.perm[tile.begin + i] : tile.begin + i) : -1;
+  for (int t = run.lo + tid / GRANULE, s = list.segment; t < run.hi; t += SK_THREADS / GRANULE) {
+    const Tile granule = tile_of<GRANULE>(list, run, t, &s);
+    const int i = tid % GRANULE;
+    if (i < granule.rows) s_rows[(t - run.lo) * GRANULE + i] = a.perm ? a.perm[granule.begin + i] : granule.begin + i;
   }
   if (warp == 8) tmem_alloc(smem_u32(&tmem_slot), S::TMEM);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  const int c0 = blockIdx.y * S::CHANNELS, tiles = run.hi - run.lo;
+  const int c0 = blockIdx.y * S::CHANNELS;
   const int pairs = min(PAIRS, (a.dim - c0 + 127) / 128);  // of 128 channels; what the last has too many reads as zeros
-  int segment = list.segment;
+  RunWalk walk(list, run);
 
   if (warp >= 4 && warp < 8) {
     // ---- rows
-    copy_rows<SK_STAGES, true>(a.act, true, a.stride, a.dim, c0, pairs, tiles, s_rows, smem_u32(smem), full, empty, tid - 128, a.check_word, abort_flag);
+    copy_rows<SK_STAGES, true>(a.act, true, a.stride, a.dim, c0, pairs, walk, s_rows, smem_u32(smem), full, empty, tid - 128, a.check_word, abort_flag);
   } else if (warp == 8) {
     // ---- products
     const uint32_t on = elect_one();
-    constexpr uint32_t ID_DOWN = BF16_F32 | columns(RP), ID_OUTER = BF16_F32 | A_BY_COLUMNS | columns(3 * RP);
+    constexpr uint32_t ID_DOWN = BF16_F32 | columns(RP), ID_OUTER = BF16_F32 | A_BY_COLUMNS | B_BY_COLUMNS | columns(3 * RP);
     const uint32_t ring = smem_u32(smem), factor = smem_u32(s_factor), vecs = smem_u32(s_vec);
     bool ok = true;
     int it = 0, piece = 0;  // segments of the run so far
-    for (int t = 0; t < tiles && ok; ++t) {
-      const int buf = t % S::VEC_BUFS;
-      const Tile tile = tile_of<STREAM_ROWS>(list, run, run.lo + t, &segment);
-      if (DOWN && tile.starts) ok = mbar_wait_warp(ready, piece & 1, a.check_word, abort_flag);
+    for (int t = 0; walk.more() && ok; ++t) {
+      const int buf = t % VEC_BUFS;
+      const RunTile tile = walk.next();
+      if (DOWN && tile.starts) ok = mbar_wait_warp(ready + 8 * (piece & 1), (piece >> 1) & 1, a.check_word, abort_flag);
       if (OUTER && tile.starts && ok) ok = mbar_wait_warp(d2_empty, (piece & 1) ^ 1, a.check_word, abort_flag);
-      if (OUTER && ok) ok = mbar_wait_warp(vec_full + 8 * buf, (t / S::VEC_BUFS) & 1, a.check_word, abort_flag);
+      if (OUTER && ok) ok = mbar_wait_warp(vec_full + 8 * buf, (t / VEC_BUFS) & 1, a.check_word, abort_flag);
       if (DOWN && ok) ok = mbar_wait_warp(d1_empty + 8 * (t & 1), ((t >> 1) & 1) ^ 1, a.check_word, abort_flag);
       for (int p = 0; p < pairs && ok; ++p, ++it) {
         const int s = it % SK_STAGES;
@@ -261,13 +271,13 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
 #pragma unroll
           for (int k = 0; k < 8; ++k)  // 16 channels each
             umma_f16_ss_if(on, tmem + (t & 1) * RP, umma_desc(stage + k / 4 * TILE + k % 4 * 32),
-                           umma_desc(factor + (2 * p + k / 4) * RP * 128 + k % 4 * 32), ID_DOWN, p > 0 || k > 0);
+                           umma_desc(factor + piece % FACTOR_BUFS * S::FACTOR + (2 * p + k / 4) * RP * 128 + k % 4 * 32), ID_DOWN, p > 0 || k > 0);
         }
         if constexpr (OUTER) {
 #pragma unroll
           for (int k = 0; k < 8; ++k)  // 16 rows each
             umma_f16_ss_if(on, tmem + S::COL_OUTER + p * 3 * RP, umma_desc_mn(stage + k * 2048, TILE),
-                           umma_desc(vecs + buf * S::VEC + k / 4 * 3 * RP * 128 + k % 4 * 32), ID_OUTER, !tile.starts || k > 0);
+                           umma_desc_mn(vecs + buf * S::VEC + k * 2048, TILE), ID_OUTER, !tile.starts || k > 0);
         }
         umma_commit_if(on, empty + 8 * s);
       }
@@ -283,46 +293,65 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     if (a.early) pdl_wait();
     pdl_trigger();
     if (tid == 0) abort_flag[PIPE_FRONT] = 0;
-    // vectors of tile t: a thread's row, as a column of the operand
-    int ahead = segment;
-    const auto put_vectors = [&](int t) {
-      const Tile tile = tile_of<STREAM_ROWS>(list, run, run.lo + t, &ahead);
-      const int buf = t % S::VEC_BUFS, row = s_rows[t * STREAM_ROWS + tid];
-      const bool live = row >= 0;
-      const float scale = a.scales ? a.scales[ahead] : 1.f;
-      const float* v = a.vec + static_cast<size_t>(live ? (a.vec_by_place ? tile.begin + tid : row) : 0) * a.rank;
-      float f[RP];
-      load_vector<RP>(v, a.rank, live, f);
-      if (!mbar_wait_warp(vec_empty + 8 * buf, ((t / S::VEC_BUFS) & 1) ^ 1, a.check_word, abort_flag)) return false;
+    // the vector of a thread's row of the next tile: asked for and cut into parts ahead, put down once its place is free
+    RunWalk ahead = walk;
+    int next = 0;
+    float f[RP];
+    float scale = 1.f;
+    const auto ask_vectors = [&] {
+      const RunTile tile = ahead.next();
+      const bool live = tid < tile.rows;
+      scale = a.scales ? a.scales[ahead.segment] : 1.f;
+      load_vector<RP>(a.vec + static_cast<size_t>(!live ? 0 : a.vec_by_place ? tile.begin + tid : s_rows[tile.list + tid]) * a.rank, a.rank, a.rank % 4 == 0, live, f);
+    };
+    const auto put_vectors = [&] {
+      const int buf = next % VEC_BUFS;
+      uint32_t part[3][RP / 2];
 #pragma unroll
       for (int r = 0; r < RP; r += 2) {
         uint32_t p[3];
         split_pair<3>(scale * f[r], scale * f[r + 1], p);
 #pragma unroll
-        for (int j = 0; j < 3; ++j) {
-          char* base = s_vec + buf * S::VEC;
-          *reinterpret_cast<uint16_t*>(base + tile_at(j * RP + r, tid, 3 * RP)) = static_cast<uint16_t>(p[j] & 0xffffu);
-          *reinterpret_cast<uint16_t*>(base + tile_at(j * RP + r + 1, tid, 3 * RP)) = static_cast<uint16_t>(p[j] >> 16);
-        }
+        for (int j = 0; j < 3; ++j) part[j][r / 2] = p[j];
       }
+      if (!mbar_wait_warp(vec_empty + 8 * buf, ((next / VEC_BUFS) & 1) ^ 1, a.check_word, abort_flag)) return false;
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+#pragma unroll
+        for (int r = 0; r < RP; r += 8)
+          *reinterpret_cast<uint4*>(s_vec + buf * S::VEC + tile_at(tid, j * RP + r, STREAM_ROWS)) =
+              make_uint4(part[j][r / 2], part[j][r / 2 + 1], part[j][r / 2 + 2], part[j][r / 2 + 3]);
       fence_async_proxy();
       mbar_arrive(vec_full + 8 * buf);
+      ++next;
       return true;
+    };
+    int factors = 0;
+    const auto bring_factor = [&](int adapter) {
+      put_factor<RP, S::CHANNELS>(s_factor + factors % FACTOR_BUFS * S::FACTOR, a.factor, a.by_channel, adapter, a.dim, a.rank, c0, tid);
+      fence_async_proxy();
+      mbar_arrive(ready + 8 * (factors & 1));
+      ++factors;
     };
     bool ok = true;
     int piece = 0;
-    if constexpr (OUTER) ok = put_vectors(0);
-    for (int t = 0; t < tiles && ok; ++t) {
-      const Tile tile = tile_of<STREAM_ROWS>(list, run, run.lo + t, &segment);
+    if constexpr (DOWN && FACTOR_BUFS == 2) bring_factor(walk.segment);
+    if constexpr (OUTER) {
+      ask_vectors();
+      ok = put_vectors();
+    }
+    for (int t = 0; walk.more() && ok; ++t) {
+      const RunTile tile = walk.next();
+      bool asked = false;
       if constexpr (DOWN) {
-        if (tile.starts) {  // the products of the tiles before are done: their vectors have been taken
-          put_factor<RP, S::CHANNELS>(s_factor, a.factor, a.by_channel, segment, a.dim, a.rank, c0, tid);
-          fence_async_proxy();
-          mbar_arrive(ready);
-        }
+        // (the products of the tiles before are done: their vectors have been taken)
+        if (FACTOR_BUFS == 1 && tile.starts) bring_factor(walk.segment);
+        if (FACTOR_BUFS == 2 && tile.ends && walk.more()) bring_factor(list_next(list, walk));
       }
       if constexpr (OUTER) {
-        if (t + 1 < tiles && S::VEC_BUFS == 2) ok = put_vectors(t + 1);
+        asked = ahead.more();
+        if (asked) ask_vectors();
+        if (asked && VEC_BUFS == 2) ok = put_vectors();
       }
       if constexpr (DOWN) {
         if (ok) ok = mbar_wait_warp(d1_full + 8 * (t & 1), (t >> 1) & 1, a.check_word, abort_flag);
@@ -356,8 +385,8 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
           if (!ok) break;
           tc_fence_after();
           const size_t size = static_cast<size_t>(a.dim) * a.rank;
-          const int share = share_of(list, run, segment, blockIdx.x);
-          float* out = share < 0 ? a.out + segment * size : a.part + share * size;
+          const int share = share_of(list, run, walk.segment, blockIdx.x);
+          float* out = share < 0 ? a.out + walk.segment * size : a.part + share * size;
           for (int p = 0; p < pairs; ++p) {
             const int c = c0 + p * 128 + tid;
 #pragma unroll 1
@@ -392,7 +421,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
           mbar_arrive(d2_empty);
           ++piece;
         }
-        if (t + 1 < tiles && S::VEC_BUFS == 1 && ok) ok = put_vectors(t + 1);
+        if (asked && VEC_BUFS == 1 && ok) ok = put_vectors();
       }
     }
   }
@@ -403,39 +432,52 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
   }
 }
 
-// 16, 32 or 64 threads per place, by the rank.
+// A thread adds four neighbouring ranks of a place.
 __global__ void __launch_bounds__(256) lowrank_sum_kernel(SumArgs a) {
   pdl_wait();
   pdl_trigger();
-  const int per_cta = a.rank > 32 ? 4 : a.rank > 16 ? 8 : 16, lanes = 256 / per_cta;
-  const int place = blockIdx.x * per_cta + threadIdx.x / lanes, r = threadIdx.x % lanes;
+  const int lanes = a.rank > 32 ? 16 : a.rank > 16 ? 8 : 4, place = blockIdx.x * (256 / lanes) + threadIdx.x / lanes, r = threadIdx.x % lanes * 4;
   if (place >= a.n || r >= a.rank) return;
   const bool mine = place >= a.off[0] && place < a.off[a.G];
   if (!mine && !a.with_none) return;
   const size_t i = static_cast<size_t>(place) * a.rank + r, plane = static_cast<size_t>(a.n) * a.rank;
-  float v = 0.f;
-  if (mine) {
+  const size_t row = a.by_row ? static_cast<size_t>(a.perm ? a.perm[place] : place) * a.rank + r : 0;
+  if (a.rank % 4 == 0) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (mine) {
 #pragma unroll 8
-    for (int p = 0; p < a.count; ++p) v += a.planes[p * plane + i];
+      for (int p = 0; p < a.count; ++p) {
+        const float4 u = *reinterpret_cast<const float4*>(a.planes + p * plane + i);
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+      }
+    }
+    *reinterpret_cast<float4*>(a.by_place + i) = v;
+    if (a.by_row) *reinterpret_cast<float4*>(a.by_row + row) = v;
+  } else {
+    for (int k = 0; k < 4 && r + k < a.rank; ++k) {
+      float v = 0.f;
+      if (mine)
+        for (int p = 0; p < a.count; ++p) v += a.planes[p * plane + i + k];
+      a.by_place[i + k] = v;
+      if (a.by_row) a.by_row[row + k] = v;
+    }
   }
-  a.by_place[i] = v;
-  if (a.by_row) a.by_row[static_cast<size_t>(a.perm ? a.perm[place] : place) * a.rank + r] = v;
 }
 
 // ---- up -----------------------------------------------------------------------------------------
 
-// Roles: warps 0-7 add base and write, in two sets that take turns at the stages, 8-11 copy base, 12 issues the products, 13-16 bring
-// factor and vectors.
+// Roles: warps 0-7 add base and write, in two sets that take turns at the stages, 8-11 copy base, 12 issues the products, 13-16
+// bring factor and vectors.
 constexpr int UP_THREADS = 544, UP_ACC = 4;  // accumulators of 128 rows x 128 channels: all of tensor memory
 
 template <int RT>
 struct Up {
-  static constexpr int RP = RT * 16, CHANNELS = stream_channels(RP), STAGES = RT == 1 ? 5 : 4;
-  static constexpr int FACTOR = CHANNELS / 64 * RP * 128;            // [rank][channels], tiles of 64 channels
+  static constexpr int RP = RT * 16, CHANNELS = stream_channels(RP), STAGES = RT == 4 ? 3 : 4;
+  static constexpr int FACTOR = CHANNELS / 64 * RP * 128;            // [rank][channels], tiles of 64 channels; two of them
   static constexpr int VEC = (2 * RP + 63) / 64 * STREAM_ROWS * 128;  // [128 rows][two parts of rank], K-major tiles of 64 values
-  static constexpr int VEC_BUFS = RT == 4 ? 1 : 2;
+  static constexpr int VEC_BUFS = RT == 1 ? 2 : 1;
   static constexpr size_t SMEM =
-      1024 + static_cast<size_t>(STAGES) * STAGE + FACTOR + VEC_BUFS * VEC + sizeof(int) * UP_RUN * STREAM_ROWS + sizeof(TileList);
+      1024 + static_cast<size_t>(STAGES) * STAGE + 2 * FACTOR + VEC_BUFS * VEC + sizeof(int) * UP_RUN * GRANULE + sizeof(TileList);
 };
 
 // y = base + s B v: the product V F of the rows' vectors (two bf16 parts, rows of the A operand) with the factor's tiles read along their
@@ -448,17 +490,17 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
   using U = Up<RT>;
   constexpr int RP = U::RP;
   extern __shared__ char smem_raw[];
-  __shared__ __align__(8) uint64_t bars[2 * U::STAGES + 2 * UP_ACC + 6];
+  __shared__ __align__(8) uint64_t bars[2 * U::STAGES + 2 * UP_ACC + 8];
   __shared__ uint32_t tmem_slot;
   __shared__ int wait_words[PIPE_WORDS];
   volatile int* abort_flag = wait_words + PIPE_ABORT;
   char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   char* s_factor = smem + U::STAGES * STAGE;
-  char* s_vec = s_factor + U::FACTOR;
+  char* s_vec = s_factor + 2 * U::FACTOR;
   int* s_rows = reinterpret_cast<int*>(s_vec + U::VEC_BUFS * U::VEC);
-  TileList& list = *reinterpret_cast<TileList*>(s_rows + UP_RUN * STREAM_ROWS);
+  TileList& list = *reinterpret_cast<TileList*>(s_rows + UP_RUN * GRANULE);
   const uint32_t full = smem_u32(bars), empty = full + 8 * U::STAGES, acc_full = empty + 8 * U::STAGES, acc_empty = acc_full + 8 * UP_ACC,
-                 vec_full = acc_empty + 8 * UP_ACC, vec_empty = vec_full + 16, ready = vec_empty + 16, factor_free = ready + 8;
+                 vec_full = acc_empty + 8 * UP_ACC, vec_empty = vec_full + 16, ready = vec_empty + 16, factor_free = ready + 16;
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
   if (tid == 0) {
     for (int i = 0; i < U::STAGES; ++i) {
@@ -472,25 +514,24 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(vec_full + 8 * i, SIDE);
       mbar_init(vec_empty + 8 * i, 1);
+      mbar_init(ready + 8 * i, SIDE);
+      mbar_init(factor_free + 8 * i, 1);
     }
-    mbar_init(ready, SIDE);
-    mbar_init(factor_free, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     wait_words[PIPE_ABORT] = 0;
     wait_words[PIPE_FRONT] = 1;  // until the vectors' warps are past their wait for the kernel in front
   }
-  const TileRun run = list_tiles<STREAM_ROWS>(list, a.off, a.segments, a.n, blockIdx.x, a.runs);
-  const int tiles = min(run.hi - run.lo, UP_RUN);  // (more only where the segments overlap)
-  if (tiles <= 0) {
+  TileRun run = list_tiles<GRANULE>(list, a.off, a.segments, a.n, blockIdx.x, a.runs);
+  run.hi = min(run.hi, run.lo + UP_RUN);  // (longer only where the segments overlap)
+  if (run.lo >= run.hi) {
     pdl_wait();
     pdl_trigger();
     return;
   }
-  for (int t = run.lo + warp, s = list.segment; t < run.lo + tiles; t += UP_THREADS / 32) {
-    const Tile tile = tile_of<STREAM_ROWS>(list, run, t, &s);
-    const int rows = s >= a.G && a.skip_none ? 0 : tile.rows;
-    for (int i = lane; i < STREAM_ROWS; i += 32)
-      s_rows[(t - run.lo) * STREAM_ROWS + i] = i < rows ? (a.perm ? a.perm[tile.begin + i] : tile.begin + i) : -1;
+  for (int t = run.lo + tid / GRANULE, s = list.segment; t < run.hi; t += UP_THREADS / GRANULE) {
+    const Tile granule = tile_of<GRANULE>(list, run, t, &s);
+    const int i = tid % GRANULE;
+    if (i < granule.rows) s_rows[(t - run.lo) * GRANULE + i] = s >= a.G && a.skip_none ? -1 : a.perm ? a.perm[granule.begin + i] : granule.begin + i;
   }
   if (warp == 12) tmem_alloc(smem_u32(&tmem_slot), 512);
   tc_fence_before();
@@ -498,15 +539,16 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   const int c0 = blockIdx.y * U::CHANNELS, pairs = min(U::CHANNELS / 128, (a.dim - c0 + 127) / 128);
-  int segment = list.segment;
+  RunWalk walk(list, run);
 
   if (warp < 8) {
     const int set = warp >> 2, r0 = (warp & 3) * 32, own = r0 + lane;  // rows of the warp; the lane's
     bool ok = true;
     int it = 0;
     bool waited = false;
-    for (int t = 0; t < tiles && ok; ++t) {
-      const bool any = s_rows[t * STREAM_ROWS + r0] >= 0;  // rows come first
+    while (walk.more() && ok) {
+      const RunTile tile = walk.next();
+      const bool any = r0 < tile.rows;
       for (int p = 0; p < pairs; ++p, ++it) {
         if ((it & 1) != set) continue;
         const int s = it % U::STAGES, b = it % UP_ACC;
@@ -546,7 +588,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
             if (c < a.dim) {
 #pragma unroll
               for (int j = 0; j < 8; ++j) {
-                const int r = r0 + (lane >> 3) + 4 * j, at = s_rows[t * STREAM_ROWS + r];
+                const int r = r0 + (lane >> 3) + 4 * j, at = r < tile.rows ? s_rows[tile.list + r] : -1;
                 const uint4 u = *reinterpret_cast<const uint4*>(stage + tile_at(r, h * 64 + (lane & 7) * 8, STREAM_ROWS));
                 if (at >= 0) *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(at) * a.stride + c) = u;
               }
@@ -560,17 +602,17 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
       }
     }
   } else if (warp < 12) {
-    copy_rows<U::STAGES, false>(a.base ? a.base : a.out, a.base != nullptr, a.stride, a.dim, c0, pairs, tiles, s_rows, smem_u32(smem), full, empty,
+    copy_rows<U::STAGES, false>(a.base ? a.base : a.out, a.base != nullptr, a.stride, a.dim, c0, pairs, walk, s_rows, smem_u32(smem), full, empty,
                                 tid - 256, a.check_word, abort_flag);
   } else if (warp == 12) {
     const uint32_t on = elect_one();
     const uint32_t factor = smem_u32(s_factor), vecs = smem_u32(s_vec);
     bool ok = true;
     int it = 0, piece = 0;
-    for (int t = 0; t < tiles && ok; ++t) {
+    for (int t = 0; walk.more() && ok; ++t) {
       const int buf = t % U::VEC_BUFS;
-      const Tile tile = tile_of<STREAM_ROWS>(list, run, run.lo + t, &segment);
-      if (tile.starts) ok = mbar_wait_warp(ready, piece & 1, a.check_word, abort_flag);
+      const RunTile tile = walk.next();
+      if (tile.starts) ok = mbar_wait_warp(ready + 8 * (piece & 1), (piece >> 1) & 1, a.check_word, abort_flag);
       if (ok) ok = mbar_wait_warp(vec_full + 8 * buf, (t / U::VEC_BUFS) & 1, a.check_word, abort_flag);
       for (int p = 0; p < pairs && ok; ++p, ++it) {
         const int b = it % UP_ACC;
@@ -583,29 +625,30 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
           for (int k = 0; k < RT; ++k) {  // 16 ranks each
             const int at = part * RP + k * 16;
             umma_f16_ss_if(on, tmem + b * 128, umma_desc(vecs + buf * U::VEC + at / 64 * TILE + at % 64 * 2),
-                           umma_desc_mn(factor + 2 * p * RP * 128 + k * 2048, RP * 128), BF16_F32 | B_BY_COLUMNS | columns(128), part == 0 || k > 0);
+                           umma_desc_mn(factor + (piece & 1) * U::FACTOR + 2 * p * RP * 128 + k * 2048, RP * 128), BF16_F32 | B_BY_COLUMNS | columns(128), part == 0 || k > 0);
           }
         umma_commit_if(on, acc_full + 8 * b);
       }
       if (!ok) break;
       umma_commit_if(on, vec_empty + 8 * buf);
-      if (tile.ends) umma_commit_if(on, factor_free);
+      if (tile.ends) umma_commit_if(on, factor_free + 8 * (piece & 1));
       piece += tile.ends;
     }
   } else {
     const int thread = tid - 13 * 32;
     bool ok = true;
     int piece = 0;
-    for (int t = 0; t < tiles && ok; ++t) {
-      const Tile tile = tile_of<STREAM_ROWS>(list, run, run.lo + t, &segment);
-      const bool none = segment >= a.G;
-      if (tile.starts) {
-        ok = mbar_wait_warp(factor_free, (piece & 1) ^ 1, a.check_word, abort_flag);
+    for (int t = 0; walk.more() && ok; ++t) {
+      const RunTile tile = walk.next();
+      const bool none = walk.segment >= a.G;
+      if (tile.starts) {  // ahead of the products of the segment in front
+        ok = mbar_wait_warp(factor_free + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1, a.check_word, abort_flag);
         if (!ok) break;
         // the rows of no adapter: a factor of zeros
-        put_factor<RP, U::CHANNELS>(s_factor, a.factor, !a.by_rank, none ? 0 : segment, none ? 0 : a.dim, a.rank, c0, thread);
+        put_factor<RP, U::CHANNELS>(s_factor + (piece & 1) * U::FACTOR, a.factor, !a.by_rank, none ? 0 : walk.segment, none ? 0 : a.dim, a.rank, c0,
+                                          thread);
         fence_async_proxy();
-        mbar_arrive(ready);
+        mbar_arrive(ready + 8 * (piece & 1));
         ++piece;
       }
       if (t == 0) {
@@ -614,10 +657,10 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
         if (thread == 0) abort_flag[PIPE_FRONT] = 0;
       }
       const int buf = t % U::VEC_BUFS;
-      const float scale = a.scales && !none ? a.scales[segment] : 1.f;
+      const float scale = a.scales && !none ? a.scales[walk.segment] : 1.f;
       const bool live = !none && thread < tile.rows;
       float f[RP];
-      load_vector<RP>(a.vec + static_cast<size_t>(live ? tile.begin + thread : 0) * a.rank, a.rank, live, f);
+      load_vector<RP>(a.vec + static_cast<size_t>(live ? tile.begin + thread : 0) * a.rank, a.rank, a.rank % 4 == 0, live, f);
       ok = mbar_wait_warp(vec_empty + 8 * buf, ((t / U::VEC_BUFS) & 1) ^ 1, a.check_word, abort_flag);
       if (!ok) break;
 #pragma unroll
@@ -676,7 +719,7 @@ cudaError_t launch_lowrank_stream(const StreamArgs& a, cudaStream_t st) {
 }
 
 cudaError_t launch_lowrank_sum(const SumArgs& a, cudaStream_t st) {
-  const int per_cta = a.rank > 32 ? 4 : a.rank > 16 ? 8 : 16;
+  const int per_cta = a.rank > 32 ? 16 : a.rank > 16 ? 32 : 64;
   return launch_chain(lowrank_sum_kernel, dim3((a.n + per_cta - 1) / per_cta), dim3(256), 0, st, a);
 }
 
