@@ -17,12 +17,19 @@ namespace emoe {
 namespace {
 
 constexpr int ROWS_THREADS = 256;
+// CTAs per SM that the gather's registers are cut for: the rows in flight are what its speed goes by.  us without / with: 8192 tokens of 4096, two
+// picks 37.3/35.2 (six; eight spill: 38.5), with products 61.7/48.0 (five; six 51.4); 16384 tokens of 2048, eight picks 113.9/99.2.
+__host__ __device__ constexpr int gather_ctas(int picks, bool dots) { return picks >= 8 ? (dots ? 2 : 4) : picks == 2 && !dots ? 6 : 5; }
+// ... and the spread's: 8192 tokens of 4096, two picks 40.2/38.3 (six / eight), with products 66.9/55.3; 16384 tokens of 2048, eight picks 122/116; with
+// products, 8192 tokens, 117/98.
+__host__ __device__ constexpr int spread_ctas(int picks, bool dots) { return dots ? (picks > 2 ? 3 : 5) : picks > 2 ? 5 : 8; }
 
 struct RowsArgs {
   const void* in;    // spread: tokens; gather: rows
   const void* with;  // the other factor of the products: spread: rows, gather: tokens
   void* out;         // spread: rows; gather: tokens
   float* dots;       // [T][top_k]
+  int32_t* perm;     // spread: written too (null: no)
   const int32_t* slots;
   const float* weights;  // null: 1
   int T, d, top_k, threads_per_token;
@@ -75,7 +82,7 @@ __device__ __forceinline__ void write_dots(const RowsArgs& a, float (&dot)[KM], 
 }
 
 template <typename RowT, typename TokT, int VEC, int KM, bool DOTS>
-__global__ void __launch_bounds__(ROWS_THREADS) spread_kernel(RowsArgs a) {
+__global__ void __launch_bounds__(ROWS_THREADS, spread_ctas(KM, DOTS)) spread_kernel(RowsArgs a) {
   __shared__ float s_dots[DOTS ? ROWS_THREADS / 32 : 1][KM];
   pdl_wait();
   pdl_trigger();
@@ -85,8 +92,15 @@ __global__ void __launch_bounds__(ROWS_THREADS) spread_kernel(RowsArgs a) {
   if (t < a.T) {
     Pairs<KM> pairs;
     pairs.load(a, t);
+    if constexpr (!DOTS) {
+      if (a.perm) {
+#pragma unroll
+        for (int j = 0; j < KM; ++j)
+          if (in_token == j && pairs.slot[j] >= 0) a.perm[pairs.slot[j]] = t * a.top_k + j;
+      }
+    }
     const TokT* x = static_cast<const TokT*>(a.in) + static_cast<size_t>(t) * a.token_stride;
-    constexpr int U = KM > 2 && DOTS ? 1 : 2;  // pieces asked for together
+    constexpr int U = DOTS ? (KM > 2 ? 1 : 2) : VEC <= 2 ? 8 : 2;  // pieces asked for together
     for (int i0 = in_token * VEC; i0 < a.d; i0 += tpt * VEC * U) {
       Piece<TokT, VEC> px[U];
       Piece<RowT, VEC> pr[U][DOTS ? KM : 1];
@@ -128,7 +142,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) spread_kernel(RowsArgs a) {
 }
 
 template <typename RowT, typename TokT, int VEC, int KM, bool DOTS>
-__global__ void __launch_bounds__(ROWS_THREADS) gather_kernel(RowsArgs a) {
+__global__ void __launch_bounds__(ROWS_THREADS, gather_ctas(KM, DOTS)) gather_kernel(RowsArgs a) {
   __shared__ float s_dots[DOTS ? ROWS_THREADS / 32 : 1][KM];
   pdl_wait();
   pdl_trigger();
@@ -139,7 +153,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) gather_kernel(RowsArgs a) {
     Pairs<KM> pairs;
     pairs.load(a, t);
     TokT* y = static_cast<TokT*>(a.out) + static_cast<size_t>(t) * a.token_stride;
-    constexpr int U = KM >= 8 ? 1 : KM == 4 ? 2 : 4 / (DOTS ? 2 : 1);  // pieces of every row asked for together
+    constexpr int U = KM == 1 ? 4 : KM == 2 && !(DOTS && VEC == 1) ? 2 : 1;  // pieces of every row asked for together
     for (int i0 = in_token * VEC; i0 < a.d; i0 += tpt * VEC * U) {
       Piece<RowT, VEC> pr[U][KM];
       Piece<TokT, VEC> px[DOTS ? U : 1];
@@ -181,15 +195,14 @@ __global__ void __launch_bounds__(ROWS_THREADS) gather_kernel(RowsArgs a) {
 
 // ---- the order --------------------------------------------------------------------------------
 
-// Stable counting sort by one cluster of up to eight CTAs.  A warp owns a run of consecutive pairs: it counts them by expert
-// (match gives the lanes of an expert and their ranks), the counts of all warps in front of it, of its CTA and of the CTAs before (read
+// Stable counting sort by one cluster of up to eight CTAs.  A warp owns a run of consecutive pairs: it counts them by expert, the counts of all warps in front of it, of its CTA and of the CTAs before (read
 // over distributed shared memory), are its first places, and a second walk hands them out.  Two cluster-wide waits,
 // no order-dependent atomics.  keep_rest: ids outside [0, E - 1) count as E - 1.
-constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CLUSTER = 8, SORT_STEPS = 8;
+constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_CLUSTER = 8, SORT_STEPS = 16;
 
 __global__ void __launch_bounds__(SORT_THREADS)
     sort_pairs_kernel(const int32_t* __restrict__ ids, int n, int E, bool keep_rest, int32_t* __restrict__ counts, int32_t* __restrict__ off,
-                      int32_t* __restrict__ perm, int32_t* __restrict__ slot_of_pair, int* __restrict__ check_word) {
+                      int32_t* __restrict__ perm, bool write_perm, int32_t* __restrict__ slot_of_pair, int* __restrict__ check_word) {
   extern __shared__ int first[];  // [SORT_WARPS][E]: pairs of a warp by expert, then the next place of each
   __shared__ int hist[EMOE_MAX_EXPERTS + 1], s_off[EMOE_MAX_EXPERTS + 2];
   cg::cluster_group cluster = cg::this_cluster();
@@ -198,13 +211,16 @@ __global__ void __launch_bounds__(SORT_THREADS)
   const int run = (n + ctas * SORT_THREADS - 1) / (ctas * SORT_THREADS) * 32;
   const int begin = (rank * SORT_WARPS + warp) * run;
   int* mine = first + warp * E;
+  const int bits = 32 - __clz(E - 1 > 0 ? E - 1 : 1);
   const int named = keep_rest ? E - 1 : E, rest = keep_rest ? E - 1 : -1;
   for (int i = tid; i < SORT_WARPS * E; i += SORT_THREADS) first[i] = 0;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
   bool bad = false;
-  int id[SORT_STEPS];  // ids of eight steps are asked for together; a run of no more is read once
+  // Ids of sixteen steps are asked for together.  A step's lanes of one expert come from one ballot per bit of the id (match.any takes a
+  // round per different value: 43 us instead of 9 for 131072 pairs of 128 experts).  place: rank among them and, in the first of them, how many.
+  int id[SORT_STEPS], place[SORT_STEPS];
   const auto load = [&](int p0) {
 #pragma unroll
     for (int i = 0; i < SORT_STEPS; ++i) {
@@ -216,35 +232,45 @@ __global__ void __launch_bounds__(SORT_THREADS)
         id[i] = rest;
       }
     }
+#pragma unroll
+    for (int i = 0; i < SORT_STEPS; ++i) {
+      if (p0 + 32 * i >= begin + run || p0 + 32 * i >= n) break;
+      unsigned same = __ballot_sync(0xffffffffu, id[i] >= 0);
+      for (int b = 0; b < bits; ++b) {
+        const unsigned set = __ballot_sync(0xffffffffu, id[i] >> b & 1);
+        same &= (id[i] >> b & 1) ? set : ~set;
+      }
+      const int rank_in = __popc(same & ((1u << lane) - 1u));
+      place[i] = rank_in == 0 ? __popc(same) << 8 : rank_in;
+    }
   };
   for (int p0 = begin; p0 < begin + run && p0 < n; p0 += 32 * SORT_STEPS) {
     load(p0);
 #pragma unroll
     for (int i = 0; i < SORT_STEPS; ++i) {
       if (p0 + 32 * i >= begin + run || p0 + 32 * i >= n) break;
-      const unsigned same = __match_any_sync(0xffffffffu, id[i]);
-      if (id[i] >= 0 && lane == __ffs(same) - 1) mine[id[i]] += __popc(same);
+      if (id[i] >= 0 && place[i] >= 256) mine[id[i]] += place[i] >> 8;
       __syncwarp();
     }
   }
   if (bad) atomicOr(check_word, CHECK_BAD_EXPERT_ID);
   __syncthreads();
-  int of_warp[SORT_WARPS];  // of expert tid
   if (tid < E) {
     int sum = 0;
-#pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) of_warp[w] = first[w * E + tid];
-#pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) sum += of_warp[w];
+#pragma unroll 8
+    for (int w = 0; w < SORT_WARPS; ++w) sum += first[w * E + tid];
     hist[tid] = sum;
   }
   cluster.sync();
   int before = 0, total = 0;
   if (tid < E) {
-    for (int r = 0; r < ctas; ++r) {
-      const int c = cluster.map_shared_rank(hist, r)[tid];
-      if (r < rank) before += c;
-      total += c;
+    int of_cta[SORT_CLUSTER];
+#pragma unroll
+    for (int r = 0; r < SORT_CLUSTER; ++r) of_cta[r] = r < ctas ? cluster.map_shared_rank(hist, r)[tid] : 0;
+#pragma unroll
+    for (int r = 0; r < SORT_CLUSTER; ++r) {
+      if (r < rank) before += of_cta[r];
+      total += of_cta[r];
     }
     s_off[tid + 1] = total;
     if (rank == 0 && counts) counts[tid] = total;
@@ -268,10 +294,15 @@ __global__ void __launch_bounds__(SORT_THREADS)
   __syncthreads();
   if (tid < E) {
     int next = s_off[tid] + before;
+    for (int w0 = 0; w0 < SORT_WARPS; w0 += 8) {
+      int c[8];
 #pragma unroll
-    for (int w = 0; w < SORT_WARPS; ++w) {
-      first[w * E + tid] = next;
-      next += of_warp[w];
+      for (int w = 0; w < 8; ++w) c[w] = first[(w0 + w) * E + tid];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        first[(w0 + w) * E + tid] = next;
+        next += c[w];
+      }
     }
   }
   if (rank == 0)
@@ -285,15 +316,14 @@ __global__ void __launch_bounds__(SORT_THREADS)
     for (int i = 0; i < SORT_STEPS; ++i) {
       if (p0 + 32 * i >= begin + run || p0 + 32 * i >= n) break;
       const int p = p0 + 32 * i + lane, e = id[i];
-      const unsigned same = __match_any_sync(0xffffffffu, e);
       int pos = -1;
       if (e >= 0) {
-        pos = mine[e] + __popc(same & ((1u << lane) - 1u));
-        perm[pos] = p;
+        pos = mine[e] + (place[i] & 255);
+        if (write_perm) perm[pos] = p;
       }
       if (p < n && slot_of_pair) slot_of_pair[p] = pos;
       __syncwarp();
-      if (e >= 0 && lane == __ffs(same) - 1) mine[e] += __popc(same);
+      if (e >= 0 && place[i] >= 256) mine[e] += place[i] >> 8;
       __syncwarp();
     }
   }
@@ -301,14 +331,15 @@ __global__ void __launch_bounds__(SORT_THREADS)
 }
 
 // Few pairs: order and rows in one launch.  A CTA per token counts, for each of its pairs, the pairs in front of it in the order (all ids,
-// from L2) while its row is on the way; one CTA more writes counts, offsets and the places of no pair.
+// from L2) while its row is on the way; one CTA more writes counts, offsets and the places of no pair.  us, order by the cluster and rows behind
+// it / this, tokens of 4096, two picks: 64 tokens 5.3/2.0, 512 tokens 7.6/3.8, 1024 tokens 9.4/6.1, 2048 tokens 14.6/15.0.
 constexpr int DISPATCH_ONE_PAIRS = 2048;
-template <typename RowT, typename TokT, int VEC>
+template <typename RowT, typename TokT, int VEC, int KM>
 __global__ void __launch_bounds__(ROWS_THREADS)
     dispatch_one_kernel(RowsArgs a, const int32_t* __restrict__ ids, int E, int32_t* __restrict__ counts, int32_t* __restrict__ off,
                         int32_t* __restrict__ perm, int32_t* __restrict__ slot_of_pair, int* __restrict__ check_word) {
   __shared__ int s_cnt[EMOE_MAX_EXPERTS + 1];
-  __shared__ int s_part[ROWS_THREADS / 32][EMOE_MAX_TOP_K];
+  __shared__ int s_part[ROWS_THREADS / 32][KM];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, P = a.T * a.top_k;
   pdl_wait();
   pdl_trigger();
@@ -358,9 +389,9 @@ __global__ void __launch_bounds__(ROWS_THREADS)
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if ((tid + u * ROWS_THREADS) * VEC < a.d) px[u] = load_piece<TokT, VEC>(x + (tid + u * ROWS_THREADS) * VEC);
-  int e[EMOE_MAX_TOP_K], in_front[EMOE_MAX_TOP_K];
+  int e[KM], in_front[KM];
 #pragma unroll
-  for (int j = 0; j < EMOE_MAX_TOP_K; ++j) {
+  for (int j = 0; j < KM; ++j) {
     in_front[j] = 0;
     e[j] = j < a.top_k ? ids[t * a.top_k + j] : -1;
     if (e[j] >= E) e[j] = -1;
@@ -369,20 +400,20 @@ __global__ void __launch_bounds__(ROWS_THREADS)
     const int eq = ids[q];
     if (eq < 0 || eq >= E) continue;
 #pragma unroll
-    for (int j = 0; j < EMOE_MAX_TOP_K; ++j)
+    for (int j = 0; j < KM; ++j)
       if (j < a.top_k) in_front[j] += eq < e[j] || (eq == e[j] && q < t * a.top_k + j);
   }
 #pragma unroll
-  for (int j = 0; j < EMOE_MAX_TOP_K; ++j)
+  for (int j = 0; j < KM; ++j)
     if (j < a.top_k) {
       const int sum = __reduce_add_sync(0xffffffffu, in_front[j]);
       if (lane == 0) s_part[warp][j] = sum;
     }
   __syncthreads();
-  int slot[EMOE_MAX_TOP_K];
-  float w[EMOE_MAX_TOP_K];
+  int slot[KM];
+  float w[KM];
 #pragma unroll
-  for (int j = 0; j < EMOE_MAX_TOP_K; ++j) {
+  for (int j = 0; j < KM; ++j) {
     slot[j] = -1;
     w[j] = 1.f;
     if (j < a.top_k && e[j] >= 0) {
@@ -407,7 +438,7 @@ __global__ void __launch_bounds__(ROWS_THREADS)
       float f[VEC];
       widen<TokT, VEC>(px[u], f);
 #pragma unroll
-      for (int j = 0; j < EMOE_MAX_TOP_K; ++j) {
+      for (int j = 0; j < KM; ++j) {
         if (slot[j] < 0) continue;
         float o[VEC];
 #pragma unroll
@@ -546,17 +577,18 @@ struct Tag {
   using type = T;
 };
 
-// f(rows' type, tokens' type, values per piece): wide pieces where every address and the row length allow them
+// f(rows' type, tokens' type, values per piece): 16 bytes of a row where every address and the row length allow them, else two values, else one
+enum Width { ONE, TWO, WIDE };
 template <typename F>
-cudaError_t by_types(int row_dtype, int token_dtype, bool wide, F&& f) {
-  const bool rb = row_dtype == EMOE_DTYPE_BF16, tb = token_dtype == EMOE_DTYPE_BF16;
-  const auto one = std::integral_constant<int, 1>();
-  const auto four = std::integral_constant<int, 4>();
-  const auto eight = std::integral_constant<int, 8>();
-  if (rb && tb) return wide ? f(Tag<__nv_bfloat16>(), Tag<__nv_bfloat16>(), eight) : f(Tag<__nv_bfloat16>(), Tag<__nv_bfloat16>(), one);
-  if (rb) return wide ? f(Tag<__nv_bfloat16>(), Tag<float>(), eight) : f(Tag<__nv_bfloat16>(), Tag<float>(), one);
-  if (tb) return wide ? f(Tag<float>(), Tag<__nv_bfloat16>(), four) : f(Tag<float>(), Tag<__nv_bfloat16>(), one);
-  return wide ? f(Tag<float>(), Tag<float>(), four) : f(Tag<float>(), Tag<float>(), one);
+cudaError_t by_types(int row_dtype, int token_dtype, Width width, F&& f) {
+  const auto by_width = [&](auto row, auto tok) -> cudaError_t {
+    constexpr int MOST = sizeof(typename decltype(row)::type) == 2 ? 8 : 4;
+    if (width == WIDE) return f(row, tok, std::integral_constant<int, MOST>());
+    return width == TWO ? f(row, tok, std::integral_constant<int, 2>()) : f(row, tok, std::integral_constant<int, 1>());
+  };
+  const bool tb = token_dtype == EMOE_DTYPE_BF16;
+  if (row_dtype == EMOE_DTYPE_BF16) return tb ? by_width(Tag<__nv_bfloat16>(), Tag<__nv_bfloat16>()) : by_width(Tag<__nv_bfloat16>(), Tag<float>());
+  return tb ? by_width(Tag<float>(), Tag<__nv_bfloat16>()) : by_width(Tag<float>(), Tag<float>());
 }
 
 int threads_per_token(int d, int vec) {
@@ -564,16 +596,18 @@ int threads_per_token(int d, int vec) {
   return pieces <= 32 ? 32 : pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256;
 }
 
-bool wide_rows(const emoe_dispatch_desc& D, const RowsArgs& a) {
-  const int vec = D.row_dtype == EMOE_DTYPE_BF16 ? 8 : 4;
-  const size_t tok_bytes = vec * dtype_size(D.token_dtype), tok_align = tok_bytes < 16 ? tok_bytes : 16;
-  if (a.d % vec != 0 || a.row_stride * dtype_size(D.row_dtype) % 16 != 0 || a.token_stride * dtype_size(D.token_dtype) % tok_align != 0) return false;
-  return true;
+Width width_of(const emoe_dispatch_desc& D, const RowsArgs& a, const void* rows, const void* rows_too, const void* tokens, const void* tokens_too) {
+  const size_t rz = dtype_size(D.row_dtype), tz = dtype_size(D.token_dtype);
+  const auto fits = [&](int vec) {
+    const size_t ra = vec * rz < 16 ? vec * rz : 16, ta = vec * tz < 16 ? vec * tz : 16;
+    return a.d % vec == 0 && a.row_stride * rz % ra == 0 && a.token_stride * tz % ta == 0 && ptr_aligned(rows, ra) && ptr_aligned(rows_too, ra) &&
+           ptr_aligned(tokens, ta) && ptr_aligned(tokens_too, ta);
+  };
+  return fits(rz == 2 ? 8 : 4) ? WIDE : fits(2) ? TWO : ONE;
 }
 
 cudaError_t launch_gather(const emoe_dispatch_desc& D, RowsArgs a, cudaStream_t st) {
-  const size_t tok_align = (D.row_dtype == EMOE_DTYPE_BF16 ? 8 : 4) * dtype_size(D.token_dtype) < 16 ? 8 : 16;
-  const bool wide = wide_rows(D, a) && ptr_aligned(a.in, 16) && ptr_aligned(a.out, tok_align) && (!a.with || ptr_aligned(a.with, tok_align));
+  const Width wide = width_of(D, a, a.in, nullptr, a.out, a.with);
   return by_types(D.row_dtype, D.token_dtype, wide, [&](auto row, auto tok, auto vec) {
     using RowT = typename decltype(row)::type;
     using TokT = typename decltype(tok)::type;
@@ -590,8 +624,7 @@ cudaError_t launch_gather(const emoe_dispatch_desc& D, RowsArgs a, cudaStream_t 
 
 // the picks known: slots given
 cudaError_t launch_spread(const emoe_dispatch_desc& D, RowsArgs a, cudaStream_t st) {
-  const size_t tok_align = (D.row_dtype == EMOE_DTYPE_BF16 ? 8 : 4) * dtype_size(D.token_dtype) < 16 ? 8 : 16;
-  const bool wide = wide_rows(D, a) && ptr_aligned(a.in, tok_align) && ptr_aligned(a.out, 16) && (!a.with || ptr_aligned(a.with, 16));
+  const Width wide = width_of(D, a, a.out, a.with, a.in, nullptr);
   return by_types(D.row_dtype, D.token_dtype, wide, [&](auto row, auto tok, auto vec) {
     using RowT = typename decltype(row)::type;
     using TokT = typename decltype(tok)::type;
@@ -606,13 +639,14 @@ cudaError_t launch_spread(const emoe_dispatch_desc& D, RowsArgs a, cudaStream_t 
 
 cudaError_t launch_dispatch_one(const emoe_dispatch_desc& D, RowsArgs a, const int32_t* ids, int32_t* counts, int32_t* off, int32_t* perm,
                                 int32_t* slots, int* check_word, cudaStream_t st) {
-  const size_t tok_align = (D.row_dtype == EMOE_DTYPE_BF16 ? 8 : 4) * dtype_size(D.token_dtype) < 16 ? 8 : 16;
-  const bool wide = wide_rows(D, a) && ptr_aligned(a.in, tok_align) && ptr_aligned(a.out, 16);
+  const Width wide = width_of(D, a, a.out, nullptr, a.in, nullptr);
   return by_types(D.row_dtype, D.token_dtype, wide, [&](auto row, auto tok, auto vec) {
     using RowT = typename decltype(row)::type;
     using TokT = typename decltype(tok)::type;
-    return launch_chain(dispatch_one_kernel<RowT, TokT, decltype(vec)::value>, dim3(a.T + 1), dim3(ROWS_THREADS), 0, st, a, ids, D.n_experts,
-                        counts, off, perm, slots, check_word);
+    const auto go = [&](auto kernel) {
+      return launch_chain(kernel, dim3(a.T + 1), dim3(ROWS_THREADS), 0, st, a, ids, D.n_experts, counts, off, perm, slots, check_word);
+    };
+    return a.top_k <= 2 ? go(dispatch_one_kernel<RowT, TokT, decltype(vec)::value, 2>) : go(dispatch_one_kernel<RowT, TokT, decltype(vec)::value, 8>);
   });
 }
 
@@ -654,7 +688,7 @@ bool words_aligned(const P*... p) {
 
 }  // namespace
 
-cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32_t* counts, int32_t* off, int32_t* perm, int32_t* slot_of_pair,
+cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32_t* counts, int32_t* off, int32_t* perm, bool write_perm, int32_t* slot_of_pair,
                               int* check_word, cudaStream_t st) {
   const int ctas = n <= 2 * SORT_THREADS ? 1 : SORT_CLUSTER;
   cudaLaunchConfig_t cfg = {};
@@ -670,7 +704,7 @@ cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = g_pdl_enabled ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, sort_pairs_kernel, ids, n, E, rest, counts, off, perm, slot_of_pair, check_word);
+  return cudaLaunchKernelEx(&cfg, sort_pairs_kernel, ids, n, E, rest, counts, off, perm, write_perm, slot_of_pair, check_word);
 }
 
 }  // namespace emoe
@@ -704,8 +738,9 @@ int emoe_dispatch(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* x, 
     EMOE_CALL(ctx, launch_dispatch_one(*desc, a, ids, out_counts, out_off, out_perm, out_slot_of_pair, ctx_check_word(ctx), st));
     return EMOE_OK;
   }
-  EMOE_CALL(ctx, launch_sort_pairs(ids, T * desc->top_k, desc->n_experts, false, out_counts, out_off, out_perm, out_slot_of_pair,
-                                   ctx_check_word(ctx), st));
+  EMOE_CALL(ctx, launch_sort_pairs(ids, T * desc->top_k, desc->n_experts, false, out_counts, out_off, out_perm, false,
+                                   out_slot_of_pair, ctx_check_word(ctx), st));
+  a.perm = out_perm;  // scattered words: from all SMs, not from the eight of the sort
   EMOE_CALL(ctx, launch_spread(*desc, a, st));
   return EMOE_OK;
 }

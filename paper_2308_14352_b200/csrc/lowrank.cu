@@ -501,9 +501,9 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
   const T* act = static_cast<const T*>(a.act[which]);
   const float* vec = a.vec[which];
   float acc[4][NR][4] = {};
-  for (int t = run.lo, segment = list.segment; t < run.hi; ++t) {
-    const Tile tile = tile_of<GR_ROWS>(list, run, t, &segment);
-    const int rows = tile.rows;
+  for (RunWalk<GR_ROWS> walk(list, run); walk.more();) {
+    const Tile tile = walk.next();
+    const int rows = tile.rows, segment = walk.segment;
     const float scale = which == 0 && a.scales ? a.scales[segment] : 1.f;
     __syncthreads();  // the vectors of the rows before have been used
     for (int i = tid; i < GR_ROWS; i += LR_THREADS) s_rows[i] = i < rows ? (a.perm ? a.perm[tile.begin + i] : tile.begin + i) : -1;
@@ -659,10 +659,10 @@ LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n, bool back) {
     if (!back) continue;
     // 1024 rows at most per run, as accuracy goes on the streaming path
     w.runs[i] = runs_for(n, D.n_adapters, blocks_of(static_cast<int>(dim), stream ? stream_channels(D.rank) : GR_CHANNELS), GPU_SMS,
-                         stream ? GRANULE : GR_ROWS, stream ? STREAM_RUN : STREAM_RUN * GRANULE / GR_ROWS);
+                         stream ? STREAM_ROWS : GR_ROWS, stream ? STREAM_RUN : STREAM_RUN * STREAM_ROWS / GR_ROWS);
     // Two shares per run.  What is reserved grows with n, dim and rank alike, so that a context that is made for the largest call serves all:
-    // runs <= slots / blocks + granules / 64 + 1 and slots / blocks * dim <= slots * 512; runs <= granules.
-    const size_t tiles = (static_cast<size_t>(n) + GRANULE - 1) / GRANULE + (D.n_adapters < n ? D.n_adapters : n);
+    // runs <= slots / blocks + tiles / 8 + 1 and slots / blocks * dim <= slots * 512; runs <= tiles.
+    const size_t tiles = (static_cast<size_t>(n) + GR_ROWS - 1) / GR_ROWS + (D.n_adapters < n ? D.n_adapters : n);
     const size_t even = static_cast<size_t>(2 * GPU_SMS) * 512 + (tiles / STREAM_RUN + 2) * dim;
     o += up(sizeof(float) * 2 * (tiles * dim < even ? tiles * dim : even) * D.rank);
   }
@@ -718,7 +718,7 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
 cudaError_t launch_join(const GradArgs& a, bool stream, cudaStream_t st) {
   const size_t dim = a.dim[0] > a.dim[1] ? a.dim[0] : a.dim[1], shares = (dim * a.rank / 4 + LR_THREADS - 1) / LR_THREADS;
   const dim3 grid(a.G, static_cast<unsigned>(shares < 32 ? shares : 32), 2);
-  if (stream) return launch_chain(lowrank_join_kernel<GRANULE>, grid, dim3(LR_THREADS), 0, st, a);
+  if (stream) return launch_chain(lowrank_join_kernel<STREAM_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
   return launch_chain(lowrank_join_kernel<GR_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
 }
 
@@ -757,7 +757,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
   s.n = a.n;
   s.G = a.G;
   s.rank = a.rank;
-  s.runs = runs_for(a.n, a.G, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, GRANULE, STREAM_RUN);
+  s.runs = runs_for(a.n, a.G, blocks_of(a.in_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, STREAM_RUN);
   if (back && ga->out[0]) outer(0, &s);
   cudaError_t e = cudaSuccess;
   if (s.factor || s.vec) e = launch_lowrank_stream(s, st);
@@ -782,7 +782,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
     p.G = a.G;
     p.segments = a.segments;
     p.rank = a.rank;
-    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, stream_channels(a.rank)), GPU_SMS, GRANULE, UP_RUN);
+    p.runs = runs_for(a.n, a.segments, blocks_of(a.out_dim, stream_channels(a.rank)), GPU_SMS, STREAM_ROWS, UP_RUN);
     p.skip_none = a.skip_none;
     e = launch_lowrank_up(p, st);
     if (e != cudaSuccess) return e;
@@ -804,7 +804,7 @@ int check_lowrank(const emoe_lowrank_desc* D, int n, const int32_t* ids, const i
   if ((ids == nullptr) == (off == nullptr)) return EMOE_ERR_INVALID_ARG;
   if ((D->x_stride && D->x_stride < D->in_dim) || (D->y_stride && D->y_stride < D->out_dim)) return EMOE_ERR_INVALID_ARG;
   if (!dtype_ok(D->dtype) || D->rank > EMOE_MAX_RANK) return EMOE_ERR_UNSUPPORTED;
-  if (D->in_dim % 8 != 0 || D->out_dim % 8 != 0 || D->in_dim > 0x7fffffff / 64 || D->out_dim > 0x7fffffff / 64) return EMOE_ERR_UNSUPPORTED;
+  if (D->in_dim % 8 != 0 || D->out_dim % 8 != 0 || D->in_dim > 0x7fffffff / 256 || D->out_dim > 0x7fffffff / 256) return EMOE_ERR_UNSUPPORTED;
   if (n > 0x7fffffff / 16) return EMOE_ERR_UNSUPPORTED;
   const int64_t vec = 16 / static_cast<int64_t>(dtype_size(D->dtype));
   if (D->x_stride % vec != 0 || D->y_stride % vec != 0) return EMOE_ERR_ALIGNMENT;
@@ -874,7 +874,7 @@ int emoe_lowrank_forward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const voi
   } else if (ids) {
     if ((streams ? w.total : w.vec) > have) return EMOE_ERR_WORKSPACE;
     int32_t *off_ws = reinterpret_cast<int32_t*>(ws + w.off), *perm = reinterpret_cast<int32_t*>(ws + w.perm);
-    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, nullptr, a.check_word, st));
+    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, true, nullptr, a.check_word, st));
     a.off = off_ws;
     a.perm = perm;
     a.segments = desc->n_adapters + 1;
@@ -924,7 +924,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   a.y_stride = static_cast<size_t>(desc->x_stride ? desc->x_stride : desc->in_dim);
   a.off = off;
   if (ids) {
-    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, nullptr, a.check_word, st));
+    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, true, nullptr, a.check_word, st));
     a.off = off_ws;
     a.perm = perm;
     a.segments = desc->n_adapters + 1;

@@ -115,16 +115,40 @@ __device__ __forceinline__ TileRun list_tiles(TileList& list, const int32_t* __r
   __syncthreads();
   return {lo, min(lo + per, total), per};
 }
-// The tile `t` of a walk along a run: `segment` follows (it starts at list.segment).
 struct Tile {
-  int begin, rows;  // in the order
+  int begin, rows;    // in the order
   bool starts, ends;  // the first, the last of its segment within the run
 };
+// A walk along a run, tile by tile; `segment` is that of the last tile given.
 template <int H>
-__device__ __forceinline__ Tile tile_of(const TileList& list, const TileRun& run, int t, int* segment) {
-  while (t >= list.first[*segment + 1]) ++*segment;
-  const int s = *segment, in_segment = (t - list.first[s]) * H;
-  return {list.begin[s] + in_segment, min(H, list.rows[s] - in_segment), t == run.lo || t == list.first[s], t + 1 == run.hi || t + 1 == list.first[s + 1]};
+struct RunWalk {
+  const TileList& list;
+  int lo, hi, at, segment;
+  __device__ __forceinline__ RunWalk(const TileList& l, const TileRun& run) : list(l), lo(run.lo), hi(run.hi), at(run.lo), segment(l.segment) {}
+  __device__ __forceinline__ bool more() const { return at < hi; }
+  __device__ __forceinline__ int next_segment() const {  // while there is more
+    int s = segment;
+    while (at >= list.first[s + 1]) ++s;
+    return s;
+  }
+  __device__ __forceinline__ Tile next() {
+    segment = next_segment();
+    const int first = list.first[segment], in_segment = (at - first) * H;
+    const Tile t = {list.begin[segment] + in_segment, min(H, list.rows[segment] - in_segment), at == lo || at == first,
+                    at + 1 == hi || at + 1 == list.first[segment + 1]};
+    ++at;
+    return t;
+  }
+};
+// Lists the rows of a run of tiles of H rows: place (t - lo) * H + i holds row i of tile t, -1 beyond its last and (none_too false) for rows of no adapter.
+template <int H>
+__device__ __forceinline__ void list_rows(const TileList& list, const TileRun& run, const int32_t* __restrict__ perm, int G, bool none_too, int* s_rows) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  for (int t = run.lo + warp, s = list.segment; t < run.hi; t += warps) {
+    while (t >= list.first[s + 1]) ++s;
+    const int in_segment = (t - list.first[s]) * H, begin = list.begin[s] + in_segment, rows = s >= G && !none_too ? 0 : list.rows[s] - in_segment;
+    for (int i = lane; i < H; i += 32) s_rows[(t - run.lo) * H + i] = i >= rows ? -1 : perm ? perm[begin + i] : begin + i;
+  }
 }
 // Outer products of a segment that several runs share are joined behind the kernel, in order.  Where a run leaves its share of segment
 // s: the part of one that goes on in the next run, else of one that began before; -1: the segment is the run's alone.
@@ -137,31 +161,10 @@ __device__ __forceinline__ int share_of(const TileList& list, const TileRun& run
 
 // channels of a CTA: as many as tensor memory has room for
 __host__ __device__ constexpr int stream_channels(int rank) { return rank <= 32 ? 512 : 256; }
-constexpr int STREAM_ROWS = 128;  // rows of their tiles at most
-// The kernels' runs are counted in granules of 16 rows, so that they are even in rows, not in tiles of which some are short; a CTA cuts
-// its own run into tiles.  Granules of the longest run: how many products are added in tensor memory; how many rows a CTA lists.
-constexpr int GRANULE = 16, STREAM_RUN = 64, UP_RUN = 128;
-struct RunTile {
-  int begin, rows;    // in the order
-  int list;           // of its first row in the CTA's list of rows
-  bool starts, ends;  // the first, the last of its segment within the run
-};
-struct RunWalk {
-  const TileList& list;
-  TileRun run;
-  int at, segment;
-  __device__ __forceinline__ RunWalk(const TileList& l, const TileRun& r) : list(l), run(r), at(r.lo), segment(l.segment) {}
-  __device__ __forceinline__ bool more() const { return at < run.hi; }
-  __device__ __forceinline__ RunTile next() {
-    while (at >= list.first[segment + 1]) ++segment;
-    const int first = list.first[segment], end = min(run.hi, list.first[segment + 1]), take = min(STREAM_ROWS / GRANULE, end - at);
-    const int in_segment = (at - first) * GRANULE;
-    const RunTile t = {list.begin[segment] + in_segment, min(take * GRANULE, list.rows[segment] - in_segment), (at - run.lo) * GRANULE,
-                       at == run.lo || at == first, at + take == end};
-    at += take;
-    return t;
-  }
-};
+// Rows of their tiles, the unit of a run (finer runs, even in rows, cut more tiles short, and a short one costs little less than a full one: 16
+// rows 83 us where 128 rows take 75, 4099 rows of 16 adapters); tiles of the longest run, which is how many products are added in tensor memory, and how
+// many rows a CTA lists.
+constexpr int STREAM_ROWS = 128, STREAM_RUN = 8, UP_RUN = 16;
 
 struct StreamArgs {
   const __nv_bfloat16* act;     // rows that go by

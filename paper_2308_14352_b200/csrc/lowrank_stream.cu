@@ -42,7 +42,7 @@ __device__ __forceinline__ void copy_arrive(uint32_t bar) { asm volatile("cp.asy
 // the products of a stage would not start before those in front of it are done: 14 instead of 10 us per 67 MB).  Else threads read it
 // and the copies arrive by themselves.
 template <int STAGES, bool FOR_MMA>
-__device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted, size_t stride, int dim, int c0, int pairs, RunWalk walk, const int* s_rows,
+__device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted, size_t stride, int dim, int c0, int pairs, RunWalk<STREAM_ROWS> walk, const int* s_rows,
                                           uint32_t ring, uint32_t full, uint32_t empty, int thread, int* check_word, volatile int* abort_flag) {
   const int piece = thread & 15, row0 = thread >> 4;
   const uint32_t dst = ring + (piece >> 3) * TILE + row0 * 128 + (((piece & 7) ^ row0) << 4);
@@ -54,11 +54,11 @@ __device__ __forceinline__ void copy_rows(const __nv_bfloat16* act, bool wanted,
     mbar_arrive(full + 8 * (stage % STAGES));
   };
   while (walk.more() && ok) {
-    const RunTile tile = walk.next();
+    walk.next();
     uint32_t live = 0;
 #pragma unroll
     for (int j = 0; j < STREAM_ROWS / 8; ++j) {
-      const int r = row0 + 8 * j < tile.rows ? s_rows[tile.list + row0 + 8 * j] : -1;
+      const int r = s_rows[(walk.at - 1 - walk.lo) * STREAM_ROWS + row0 + 8 * j];
       if (r >= 0 && wanted) live |= 1u << j;
       row[j] = act + static_cast<size_t>(max(r, 0)) * stride;
     }
@@ -145,13 +145,6 @@ __device__ __forceinline__ void load_vector(const float* v, int count, bool word
   }
 }
 
-// the segment that follows in a run that has more
-__device__ __forceinline__ int list_next(const TileList& list, const RunWalk& walk) {
-  int s = walk.segment;
-  while (walk.at >= list.first[s + 1]) ++s;
-  return s;
-}
-
 constexpr uint32_t BF16_F32 = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);  // instruction descriptor: bf16 x bf16 -> fp32, M = 128
 __host__ __device__ constexpr uint32_t columns(int n) { return static_cast<uint32_t>(n / 8) << 17; }
 constexpr uint32_t A_BY_COLUMNS = 1u << 15, B_BY_COLUMNS = 1u << 16;  // operand is MN-major
@@ -173,7 +166,7 @@ struct Stream {
   // two factors where there is room: the next segment's comes in ahead (a change of segments stops the products for some 3 us else)
   __host__ __device__ static constexpr int factor_bufs(bool outer) { return RT == 1 || !outer ? 2 : 1; }
   static constexpr size_t smem(bool down, bool outer) {
-    return 1024 + static_cast<size_t>(SK_STAGES) * STAGE + (down ? factor_bufs(outer) * FACTOR : 0) + (outer ? vec_bufs(down) * VEC : 0) + sizeof(int) * STREAM_RUN * GRANULE + sizeof(TileList);
+    return 1024 + static_cast<size_t>(SK_STAGES) * STAGE + (down ? factor_bufs(outer) * FACTOR : 0) + (outer ? vec_bufs(down) * VEC : 0) + sizeof(int) * STREAM_RUN * STREAM_ROWS + sizeof(TileList);
   }
 };
 
@@ -196,7 +189,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
   char* s_factor = smem + SK_STAGES * STAGE;
   char* s_vec = s_factor + (DOWN ? FACTOR_BUFS * S::FACTOR : 0);
   int* s_rows = reinterpret_cast<int*>(s_vec + (OUTER ? VEC_BUFS * S::VEC : 0));
-  TileList& list = *reinterpret_cast<TileList*>(s_rows + STREAM_RUN * GRANULE);
+  TileList& list = *reinterpret_cast<TileList*>(s_rows + STREAM_RUN * STREAM_ROWS);
   const uint32_t full = smem_u32(bars), empty = full + 8 * SK_STAGES, d1_full = empty + 8 * SK_STAGES, d1_empty = d1_full + 16,
                  vec_full = d1_empty + 16, vec_empty = vec_full + 16, ready = vec_empty + 16, d2_full = ready + 16, d2_empty = d2_full + 8;
   const int tid = threadIdx.x, warp = uniform_warp();
@@ -219,7 +212,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     wait_words[PIPE_FRONT] = a.early;
   }
   if (!a.early) pdl_wait();
-  const TileRun run = list_tiles<GRANULE>(list, a.off, a.G, a.n, blockIdx.x, a.runs);
+  const TileRun run = list_tiles<STREAM_ROWS>(list, a.off, a.G, a.n, blockIdx.x, a.runs);
   if (run.lo >= run.hi) {
     pdl_wait();
     pdl_trigger();
@@ -230,11 +223,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     if (tid == 0) atomicOr(a.check_word, CHECK_BAD_EXPERT_ID);
     return;
   }
-  for (int t = run.lo + tid / GRANULE, s = list.segment; t < run.hi; t += SK_THREADS / GRANULE) {
-    const Tile granule = tile_of<GRANULE>(list, run, t, &s);
-    const int i = tid % GRANULE;
-    if (i < granule.rows) s_rows[(t - run.lo) * GRANULE + i] = a.perm ? a.perm[granule.begin + i] : granule.begin + i;
-  }
+  list_rows<STREAM_ROWS>(list, run, a.perm, a.G, true, s_rows);
   if (warp == 8) tmem_alloc(smem_u32(&tmem_slot), S::TMEM);
   tc_fence_before();
   __syncthreads();
@@ -242,7 +231,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
   const uint32_t tmem = tmem_slot;
   const int c0 = blockIdx.y * S::CHANNELS;
   const int pairs = min(PAIRS, (a.dim - c0 + 127) / 128);  // of 128 channels; what the last has too many reads as zeros
-  RunWalk walk(list, run);
+  RunWalk<STREAM_ROWS> walk(list, run);
 
   if (warp >= 4 && warp < 8) {
     // ---- rows
@@ -256,7 +245,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     int it = 0, piece = 0;  // segments of the run so far
     for (int t = 0; walk.more() && ok; ++t) {
       const int buf = t % VEC_BUFS;
-      const RunTile tile = walk.next();
+      const Tile tile = walk.next();
       if (DOWN && tile.starts) ok = mbar_wait_warp(ready + 8 * (piece & 1), (piece >> 1) & 1, a.check_word, abort_flag);
       if (OUTER && tile.starts && ok) ok = mbar_wait_warp(d2_empty, (piece & 1) ^ 1, a.check_word, abort_flag);
       if (OUTER && ok) ok = mbar_wait_warp(vec_full + 8 * buf, (t / VEC_BUFS) & 1, a.check_word, abort_flag);
@@ -294,15 +283,15 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
     pdl_trigger();
     if (tid == 0) abort_flag[PIPE_FRONT] = 0;
     // the vector of a thread's row of the next tile: asked for and cut into parts ahead, put down once its place is free
-    RunWalk ahead = walk;
+    RunWalk<STREAM_ROWS> ahead = walk;
     int next = 0;
     float f[RP];
     float scale = 1.f;
     const auto ask_vectors = [&] {
-      const RunTile tile = ahead.next();
+      const Tile tile = ahead.next();
       const bool live = tid < tile.rows;
       scale = a.scales ? a.scales[ahead.segment] : 1.f;
-      load_vector<RP>(a.vec + static_cast<size_t>(!live ? 0 : a.vec_by_place ? tile.begin + tid : s_rows[tile.list + tid]) * a.rank, a.rank, a.rank % 4 == 0, live, f);
+      load_vector<RP>(a.vec + static_cast<size_t>(!live ? 0 : a.vec_by_place ? tile.begin + tid : s_rows[(ahead.at - 1 - run.lo) * STREAM_ROWS + tid]) * a.rank, a.rank, a.rank % 4 == 0, live, f);
     };
     const auto put_vectors = [&] {
       const int buf = next % VEC_BUFS;
@@ -341,12 +330,12 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
       ok = put_vectors();
     }
     for (int t = 0; walk.more() && ok; ++t) {
-      const RunTile tile = walk.next();
+      const Tile tile = walk.next();
       bool asked = false;
       if constexpr (DOWN) {
         // (the products of the tiles before are done: their vectors have been taken)
         if (FACTOR_BUFS == 1 && tile.starts) bring_factor(walk.segment);
-        if (FACTOR_BUFS == 2 && tile.ends && walk.more()) bring_factor(list_next(list, walk));
+        if (FACTOR_BUFS == 2 && tile.ends && walk.more()) bring_factor(walk.next_segment());
       }
       if constexpr (OUTER) {
         asked = ahead.more();
@@ -477,7 +466,7 @@ struct Up {
   static constexpr int VEC = (2 * RP + 63) / 64 * STREAM_ROWS * 128;  // [128 rows][two parts of rank], K-major tiles of 64 values
   static constexpr int VEC_BUFS = RT == 1 ? 2 : 1;
   static constexpr size_t SMEM =
-      1024 + static_cast<size_t>(STAGES) * STAGE + 2 * FACTOR + VEC_BUFS * VEC + sizeof(int) * UP_RUN * GRANULE + sizeof(TileList);
+      1024 + static_cast<size_t>(STAGES) * STAGE + 2 * FACTOR + VEC_BUFS * VEC + sizeof(int) * UP_RUN * STREAM_ROWS + sizeof(TileList);
 };
 
 // y = base + s B v: the product V F of the rows' vectors (two bf16 parts, rows of the A operand) with the factor's tiles read along their
@@ -498,7 +487,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
   char* s_factor = smem + U::STAGES * STAGE;
   char* s_vec = s_factor + 2 * U::FACTOR;
   int* s_rows = reinterpret_cast<int*>(s_vec + U::VEC_BUFS * U::VEC);
-  TileList& list = *reinterpret_cast<TileList*>(s_rows + UP_RUN * GRANULE);
+  TileList& list = *reinterpret_cast<TileList*>(s_rows + UP_RUN * STREAM_ROWS);
   const uint32_t full = smem_u32(bars), empty = full + 8 * U::STAGES, acc_full = empty + 8 * U::STAGES, acc_empty = acc_full + 8 * UP_ACC,
                  vec_full = acc_empty + 8 * UP_ACC, vec_empty = vec_full + 16, ready = vec_empty + 16, factor_free = ready + 16;
   const int tid = threadIdx.x, warp = uniform_warp(), lane = tid & 31;
@@ -521,25 +510,21 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
     wait_words[PIPE_ABORT] = 0;
     wait_words[PIPE_FRONT] = 1;  // until the vectors' warps are past their wait for the kernel in front
   }
-  TileRun run = list_tiles<GRANULE>(list, a.off, a.segments, a.n, blockIdx.x, a.runs);
+  TileRun run = list_tiles<STREAM_ROWS>(list, a.off, a.segments, a.n, blockIdx.x, a.runs);
   run.hi = min(run.hi, run.lo + UP_RUN);  // (longer only where the segments overlap)
   if (run.lo >= run.hi) {
     pdl_wait();
     pdl_trigger();
     return;
   }
-  for (int t = run.lo + tid / GRANULE, s = list.segment; t < run.hi; t += UP_THREADS / GRANULE) {
-    const Tile granule = tile_of<GRANULE>(list, run, t, &s);
-    const int i = tid % GRANULE;
-    if (i < granule.rows) s_rows[(t - run.lo) * GRANULE + i] = s >= a.G && a.skip_none ? -1 : a.perm ? a.perm[granule.begin + i] : granule.begin + i;
-  }
+  list_rows<STREAM_ROWS>(list, run, a.perm, a.G, !a.skip_none, s_rows);
   if (warp == 12) tmem_alloc(smem_u32(&tmem_slot), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   const int c0 = blockIdx.y * U::CHANNELS, pairs = min(U::CHANNELS / 128, (a.dim - c0 + 127) / 128);
-  RunWalk walk(list, run);
+  RunWalk<STREAM_ROWS> walk(list, run);
 
   if (warp < 8) {
     const int set = warp >> 2, r0 = (warp & 3) * 32, own = r0 + lane;  // rows of the warp; the lane's
@@ -547,8 +532,9 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
     int it = 0;
     bool waited = false;
     while (walk.more() && ok) {
-      const RunTile tile = walk.next();
-      const bool any = r0 < tile.rows;
+      walk.next();
+      const int* rows = s_rows + (walk.at - 1 - run.lo) * STREAM_ROWS;
+      const bool any = rows[r0] >= 0;  // (those with a row come first)
       for (int p = 0; p < pairs; ++p, ++it) {
         if ((it & 1) != set) continue;
         const int s = it % U::STAGES, b = it % UP_ACC;
@@ -588,7 +574,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
             if (c < a.dim) {
 #pragma unroll
               for (int j = 0; j < 8; ++j) {
-                const int r = r0 + (lane >> 3) + 4 * j, at = r < tile.rows ? s_rows[tile.list + r] : -1;
+                const int r = r0 + (lane >> 3) + 4 * j, at = rows[r];
                 const uint4 u = *reinterpret_cast<const uint4*>(stage + tile_at(r, h * 64 + (lane & 7) * 8, STREAM_ROWS));
                 if (at >= 0) *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(at) * a.stride + c) = u;
               }
@@ -611,7 +597,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
     int it = 0, piece = 0;
     for (int t = 0; walk.more() && ok; ++t) {
       const int buf = t % U::VEC_BUFS;
-      const RunTile tile = walk.next();
+      const Tile tile = walk.next();
       if (tile.starts) ok = mbar_wait_warp(ready + 8 * (piece & 1), (piece >> 1) & 1, a.check_word, abort_flag);
       if (ok) ok = mbar_wait_warp(vec_full + 8 * buf, (t / U::VEC_BUFS) & 1, a.check_word, abort_flag);
       for (int p = 0; p < pairs && ok; ++p, ++it) {
@@ -639,7 +625,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
     bool ok = true;
     int piece = 0;
     for (int t = 0; walk.more() && ok; ++t) {
-      const RunTile tile = walk.next();
+      const Tile tile = walk.next();
       const bool none = walk.segment >= a.G;
       if (tile.starts) {  // ahead of the products of the segment in front
         ok = mbar_wait_warp(factor_free + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1, a.check_word, abort_flag);

@@ -22,6 +22,9 @@ __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[8]) {
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[4]) {
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
 }
+__device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[1]) {
+  asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+}
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[2]) {
   asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
 }
@@ -37,6 +40,7 @@ template <typename T, int VEC>
 __device__ __forceinline__ void store_piece(T* p, const Piece<T, VEC>& r) {
   if constexpr (VEC == 1 && sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(r.w[0]);
   else if constexpr (VEC == 1) *reinterpret_cast<uint32_t*>(p) = r.w[0];
+  else if constexpr (Piece<T, VEC>::WORDS == 1) *reinterpret_cast<uint32_t*>(p) = r.w[0];
   else if constexpr (Piece<T, VEC>::WORDS == 2) *reinterpret_cast<uint2*>(p) = make_uint2(r.w[0], r.w[1]);
   else {
 #pragma unroll
@@ -112,8 +116,8 @@ inline bool ptr_aligned(const void* p, size_t a) { return reinterpret_cast<uintp
 
 // Stable counting sort of n ids by one cluster of CTAs (dispatch.cu): the outputs of emoe_permute.  counts and slot_of_pair may be null.
 // rest: ids outside [0, E - 1) are sorted into the last of the E lists, and only those other than -1 set the check word; else ids
-// outside [0, E) are dropped and set it.
-cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32_t* counts, int32_t* off, int32_t* perm, int32_t* slot_of_pair,
+// outside [0, E) are dropped and set it.  write_perm: else only the places without a pair are written.
+cudaError_t launch_sort_pairs(const int32_t* ids, int n, int E, bool rest, int32_t* counts, int32_t* off, int32_t* perm, bool write_perm, int32_t* slot_of_pair,
                               int* check_word, cudaStream_t st);
 
 }  // namespace emoe
