@@ -89,22 +89,22 @@ template <int RP, int CHANNELS>
 __device__ __forceinline__ void put_factor(char* tiles, const __nv_bfloat16* factor, bool by_channel, int adapter, int dim, int rank, int c0, int thread) {
   if (by_channel) {
     const uint16_t* f = reinterpret_cast<const uint16_t*>(factor) + (static_cast<size_t>(adapter) * dim + c0) * rank;
-    constexpr int N = CHANNELS / SIDE;
+    constexpr int N = CHANNELS / SIDE, W = RP < 32 ? 2 : 4;  // channels of a thread, words of eight ranks asked for together
     if (rank % 8 == 0) {
 #pragma unroll 1
-      for (int r0 = 0; r0 < RP; r0 += 16) {
-        uint4 w[N][2];
+      for (int r0 = 0; r0 < RP; r0 += 8 * W) {
+        uint4 w[N][W];
 #pragma unroll
         for (int j = 0; j < N; ++j)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < W; ++h) {
             const int c = thread + j * SIDE;
             w[j][h] = c0 + c < dim && r0 + 8 * h < rank ? *reinterpret_cast<const uint4*>(f + static_cast<size_t>(c) * rank + r0 + 8 * h) : make_uint4(0, 0, 0, 0);
           }
 #pragma unroll
         for (int j = 0; j < N; ++j)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < W; ++h) {
             const uint32_t v[4] = {w[j][h].x, w[j][h].y, w[j][h].z, w[j][h].w};
 #pragma unroll
             for (int i = 0; i < 8; ++i)
