@@ -455,7 +455,8 @@ __global__ void __launch_bounds__(256) lowrank_sum_kernel(SumArgs a) {
 
 // ---- up -----------------------------------------------------------------------------------------
 
-// Roles: warps 0-7 add base and write, in two sets that take turns at the stages, 8-11 copy base, 12 issues the products, 13-16
+// Roles: warps 0-7 add base and write, eight to a stage (a stage is held while they do: with four, and two sets of them, 1.6 us a stage
+// whatever its rows), 8-11 copy base, 12 issues the products, 13-16
 // bring factor and vectors.
 constexpr int UP_THREADS = 544, UP_ACC = 4;  // accumulators of 128 rows x 128 channels: all of tensor memory
 
@@ -494,11 +495,11 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
   if (tid == 0) {
     for (int i = 0; i < U::STAGES; ++i) {
       mbar_init(full + 8 * i, SIDE);
-      mbar_init(empty + 8 * i, SIDE);
+      mbar_init(empty + 8 * i, 2 * SIDE);
     }
     for (int i = 0; i < UP_ACC; ++i) {
       mbar_init(acc_full + 8 * i, 1);
-      mbar_init(acc_empty + 8 * i, SIDE);
+      mbar_init(acc_empty + 8 * i, 2 * SIDE);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(vec_full + 8 * i, SIDE);
@@ -527,7 +528,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
   RunWalk<STREAM_ROWS> walk(list, run);
 
   if (warp < 8) {
-    const int set = warp >> 2, r0 = (warp & 3) * 32, own = r0 + lane;  // rows of the warp; the lane's
+    const int h = warp >> 2, r0 = (warp & 3) * 32, own = r0 + lane;  // the warp's 64 channels and rows; the lane's row
     bool ok = true;
     int it = 0;
     bool waited = false;
@@ -536,7 +537,6 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
       const int* rows = s_rows + (walk.at - 1 - run.lo) * STREAM_ROWS;
       const bool any = rows[r0] >= 0;  // (those with a row come first)
       for (int p = 0; p < pairs; ++p, ++it) {
-        if ((it & 1) != set) continue;
         const int s = it % U::STAGES, b = it % UP_ACC;
         ok = mbar_wait_warp(full + 8 * s, (it / U::STAGES) & 1, a.check_word, abort_flag) &&
              mbar_wait_warp(acc_full + 8 * b, (it / UP_ACC) & 1, a.check_word, abort_flag);
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
         char* stage = smem + s * STAGE;
         if (any) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {  // 32 channels each
+          for (int q = 2 * h; q < 2 * h + 2; ++q) {  // 32 channels each
             uint32_t w[32];
             tmem_ld32(tmem + (static_cast<uint32_t>(r0) << 16) + b * 128 + q * 32, w);
             uint4 u[4];
@@ -568,16 +568,13 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
             }
           }
           __syncwarp();
+          const int c = c0 + p * 128 + h * 64 + (lane & 7) * 8;
+          if (c < a.dim) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int c = c0 + p * 128 + h * 64 + (lane & 7) * 8;
-            if (c < a.dim) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const int r = r0 + (lane >> 3) + 4 * j, at = rows[r];
-                const uint4 u = *reinterpret_cast<const uint4*>(stage + tile_at(r, h * 64 + (lane & 7) * 8, STREAM_ROWS));
-                if (at >= 0) *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(at) * a.stride + c) = u;
-              }
+            for (int j = 0; j < 8; ++j) {
+              const int r = r0 + (lane >> 3) + 4 * j, at = rows[r];
+              const uint4 u = *reinterpret_cast<const uint4*>(stage + tile_at(r, h * 64 + (lane & 7) * 8, STREAM_ROWS));
+              if (at >= 0) *reinterpret_cast<uint4*>(a.out + static_cast<size_t>(at) * a.stride + c) = u;
             }
           }
           __syncwarp();
