@@ -258,8 +258,9 @@ int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const i
  * one of the two is given.
  * Rows of no adapter: with ids y = base and v = 0 (nothing is touched where y is base), with off they are left as they were; they
  * take no part in dA and dB.  An id other than -1 outside [0,n_adapters) counts as -1 and sets the device check word.
- * Sums are fp32 or better; bf16 results are rounded once, fp32 tensors are multiplied with all their 24 bits (an infinite value in
- * them gives NaN); the same inputs give the same bits.
+ * Sums are fp32 or better; bf16 results are rounded once, fp32 tensors are multiplied with all their 24 bits; the same inputs give the same
+ * bits.  Infinities: bf16 rows give what the formulas give; an infinite value of an fp32 tensor or of a factor, and in dA and dB of
+ * any, may give NaN where they give an infinity.
  * Limits: rank 1 .. EMOE_MAX_RANK (any; multiples of 8 are faster), in_dim and out_dim multiples of 8, strides multiples of 16 bytes, tensors
  * 16-byte aligned. */
 typedef struct emoe_lowrank_desc {
@@ -274,8 +275,7 @@ typedef struct emoe_lowrank_desc {
 } emoe_lowrank_desc;
 
 /* Context workspace that calls of at most n rows need (0 for an invalid description): pass the maximum over what the context
- * serves to emoe_create.  Forward calls of at most 1024 rows whose tensors are not large,
- * and fp32 ones with `off`, use none. */
+ * serves to emoe_create.  Forward calls that read and write less than 32 MB of rows use none if they have `off` or at most 1024 rows. */
 size_t emoe_lowrank_workspace_bytes(const emoe_lowrank_desc* desc, int n);
 
 /* A [n_adapters][rank][in_dim], B [n_adapters][out_dim][rank]; scales NULL (1) or [n_adapters] fp32; x [n][in_dim]; y [n][out_dim];

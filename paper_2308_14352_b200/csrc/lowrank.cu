@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
   for (int i = tid; i < L::MT * 16 * RP; i += LR_THREADS) {
     const int t = i / RP, r = i % RP;
     float v = 0.f;
-    if (t < BT && adapter >= 0)
+    if (t < BT && adapter >= 0 && r < a.rank)  // (beyond the rank an infinite activation has met zeros)
       for (int c = 0; c < ctas; ++c) v += ctas > 1 ? cluster.map_shared_rank(s_part, c)[t * RP + r] : s_part[t * RP + r];
     const float scaled = scale * v;
     if (a.v && t < count && r < a.rank && t % ctas == cta) a.v[static_cast<size_t>(s_rows[t]) * a.rank + r] = BACK ? scaled : v;
@@ -619,7 +619,6 @@ __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
 
 // ---- launches -----------------------------------------------------------------------------------
 
-
 struct LowrankLayout {
   size_t off, perm, vec, planes, part[2], total;  // vec: dv, or the vectors in the order; planes: their shares
   int runs[2];                                    // of the outer products: dB, dA
@@ -634,9 +633,9 @@ int runs_for(int n, int segments, int blocks, int slots, int tile, int most) {
   return runs < tiles ? runs : tiles;
 }
 // Which bf16 calls take the streaming kernels, by the bytes of the rows read and written: they (and their launches) cost some 10 us more at the
-// start and run at the speed of memory from there on.  us, fused / streaming, 4096 -> 4096.  Forward, rank 16: 2048 rows 15.9/20.6, 3072 rows
-// 25/26; rank 64: 1024 rows 25/35, 1536 rows 35/32.  Backward, rank 16: 512 rows 29.6/30.5, 1024 rows 41/29 (1024 -> 1024: 2048 rows 21/24, 4096 rows
-// 31/28); rank 64: 256 rows 59/63, 512 rows 75/66.
+// start and run at the speed of memory from there on.  us, fused / streaming, 4096 -> 4096.  Forward, rank 16: 2048 rows 15.9/20.6 (4099 rows,
+// 4096 -> 14336, rank 32: 148/73); rank 64: 1024 rows 25/35, 1536 rows 35/32.  Backward, rank 16: 512 rows 29.6/30.5, 1024 rows 41/29
+// (1024 -> 1024: 2048 rows 21/24, 4096 rows 31/28); rank 64: 256 rows 59/63, 512 rows 75/66.
 bool takes_stream(const emoe_lowrank_desc& D, int n, bool back) {
   const double K = D.in_dim, N = D.out_dim, bytes = 2.0 * n * (back ? 3 * K + N : K + 2 * N);
   return D.dtype == EMOE_DTYPE_BF16 && bytes > (back ? (D.rank > 32 ? 12e6 : 20e6) : (D.rank > 32 ? 32e6 : 80e6));
