@@ -209,7 +209,7 @@ int emoe_permute(emoe_ctx* ctx, const int32_t* ids, int n_pairs, int E, int32_t*
  * than d (the strides below); buffers of one call must not overlap, but drows may be `rows` itself.
  * Pairs whose slot is outside [0, T*top_k) (a dropped pair has -1) take no part: their weight's gradient is 0, and rows that no pair
  * owns are neither read nor written.  These calls use no workspace: calls on different streams may overlap (a bad id sets the
- * context's one check word). */
+ * context's one check word).  Limits: T * top_k < 2^29, d < 2^25. */
 typedef struct emoe_dispatch_desc {
   int32_t d;            /* values per row */
   int32_t n_experts;    /* 1 .. EMOE_MAX_EXPERTS */
@@ -241,7 +241,7 @@ int emoe_combine_backward(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const v
  *                             picked logits; 0 for experts that are no pick
  * logits [T][E] as emoe_router_topk writes them (bias included), ids and dgates [T][top_k], dlogits [T][E] fp32 (not in place).  Picks outside
  * [0,E) set the device check word and take no part; a token whose (picked) logits are all -inf gets zeros.  The products that follow,
- * dx += dlogits W^T and dW = x^T dlogits, are plain matrix products. */
+ * dx += dlogits W^T and dW = x^T dlogits, are plain matrix products.  T < 2^29. */
 int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const int32_t* ids, const float* dgates, int top_k, int gate_mode,
                        float* dlogits, void* stream);
 
@@ -262,7 +262,7 @@ int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const i
  * bits.  Infinities: bf16 rows give what the formulas give; an infinite value of an fp32 tensor or of a factor, and in dA and dB of
  * any, may give NaN where they give an infinity.
  * Limits: rank 1 .. EMOE_MAX_RANK (any; multiples of 8 are faster), in_dim and out_dim multiples of 8, strides multiples of 16 bytes, tensors
- * 16-byte aligned. */
+ * 16-byte aligned, n < 2^27. */
 typedef struct emoe_lowrank_desc {
   int32_t n_adapters; /* 1 .. EMOE_MAX_EXPERTS */
   int32_t rank;

@@ -831,6 +831,7 @@ int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const i
   if (!logits || !ids || !dgates || !dlogits || T <= 0) return EMOE_ERR_INVALID_ARG;
   if (E < 1 || E > EMOE_MAX_EXPERTS || top_k < 1 || top_k > E || top_k > EMOE_MAX_TOP_K) return EMOE_ERR_INVALID_ARG;
   if (gate_mode != EMOE_GATE_SOFTMAX && gate_mode != EMOE_GATE_SOFTMAX_RENORM) return EMOE_ERR_UNSUPPORTED;
+  if (T > 0x7fffffff / 4) return EMOE_ERR_UNSUPPORTED;
   if (!words_aligned(logits, ids, dgates, dlogits)) return EMOE_ERR_ALIGNMENT;
   if (!ctx) return EMOE_ERR_INVALID_ARG;
   const CallScope scope(ctx);
