@@ -55,10 +55,12 @@ struct LayerDims {
 // tensor-memory allocation, prefetches into L2) while the
 // current one drains.  Device side, every kernel executes pdl_wait() before it reads or writes global memory: the inputs
 // of a call, too, may be what the call in front leaves.  pdl_trigger() lets the kernel behind it start.  Without the attribute both are no-ops.
-// Two kernels read some of their inputs earlier: ffn_umma.cu's second projection the plan, codes and scales; ffn_gemv.cu the table of
-// experts, its second projection offsets, codes and scales too.  That is sound only because the kernel DIRECTLY in front (the first
-// projection; the permutation in front of ffn_gemv.cu's first) has executed its own pdl_wait() before its trigger: what is older than that
-// kernel is then complete.  No launch may come between, and no trigger of theirs may move in front of the wait.
+// Some kernels read inputs earlier: ffn_umma.cu's second projection the plan, codes and scales; ffn_gemv.cu the table of
+// experts, its second projection offsets, codes and scales too; dispatch.cu's spread behind the sort pulls tokens to L2; lowrank_stream.cu's way up
+// and its second stream read all but the low-rank vectors, lowrank.cu's join the offsets.  That is sound only because the kernel DIRECTLY in front
+// (the first projection; the permutation in front of ffn_gemv.cu's first; the sort; the sum of the vectors or the way up; the kernel that leaves the
+// shares) has executed its own pdl_wait() before its trigger: what is older than that kernel is then complete.  No launch may come
+// between, and no trigger of theirs may move in front of the wait.
 extern thread_local bool g_pdl_enabled;
 
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
