@@ -20,7 +20,8 @@ __device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a
 }
 
 // Two fp32 values as N pairs of bf16 parts, largest first.  All parts but the last are truncated: what is left is exact, so three
-// parts are the value itself.  An infinity has no rest.
+// parts are the value itself.  Of two parts (bf16 results) an infinity is the first alone; of three (fp32 results) its rest is NaN, as is its
+// product with any zero part of the other side (the test would be a third of the split).
 template <int N>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N]) {
 #pragma unroll
@@ -32,8 +33,8 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[N]
     } else {
       part[i] = __byte_perm(ua, ub, 0x7632);
     }
-    a = isinf(a) ? 0.f : a - __uint_as_float(ua & 0xffff0000u);
-    b = isinf(b) ? 0.f : b - __uint_as_float(ub & 0xffff0000u);
+    a = N == 2 && isinf(a) ? 0.f : a - __uint_as_float(ua & 0xffff0000u);
+    b = N == 2 && isinf(b) ? 0.f : b - __uint_as_float(ub & 0xffff0000u);
   }
 }
 
