@@ -22,6 +22,7 @@ namespace cg = cooperative_groups;
 namespace emoe {
 namespace {
 
+constexpr int LR_CLUSTER = 8;      // most CTAs that share a tile
 constexpr int LR_IDS_ROWS = 1024;  // most rows whose adapters every CTA looks up by itself
 
 struct LowrankArgs {
@@ -282,31 +283,34 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
                 }
               }
         }
+        uint32_t bf[NT][PI][2];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          uint32_t bf[PI][2];
           if constexpr (sizeof(T) == 2) {
-            bf[0][0] = xw[t][2 * s];
-            bf[0][1] = xw[t][2 * s + 1];
+            bf[t][0][0] = xw[t][2 * s];
+            bf[t][0][1] = xw[t][2 * s + 1];
           } else {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               uint32_t p[PI];
               split_pair<PI>(__uint_as_float(xw[t][4 * s + 2 * half]), __uint_as_float(xw[t][4 * s + 2 * half + 1]), p);
 #pragma unroll
-              for (int i = 0; i < PI; ++i) bf[i][half] = p[i];
+              for (int i = 0; i < PI; ++i) bf[t][i][half] = p[i];
             }
           }
+        }
 #pragma unroll
-          for (int m = 0; m < RT; ++m) {
-            if constexpr (PI == 1) {
-              mma_parts<PI, PI>(acc[m][t], af[m], bf);
-            } else {  // the tensor cores cut what they add: sixteen products of fp32 values are summed by themselves, then added with rounding
-              float d[4] = {};
-              mma_parts<PI, PI>(d, af[m], bf);
+        for (int m = 0; m < RT; ++m) {
+          const uint32_t(&am)[1][PI][4] = reinterpret_cast<const uint32_t(&)[1][PI][4]>(af[m]);
+          if constexpr (PI == 1) {
+            mma_parts_of<false>(acc[m], am, bf);
+          } else {  // the tensor cores cut what they add: sixteen products of fp32 values are summed by themselves, then added with rounding
+            float d[NT][4];
+            mma_parts_of<true>(d, am, bf);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[m][t][i] += d[i];
-            }
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[m][t][i] += d[t][i];
           }
         }
       }
@@ -343,8 +347,13 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
   for (int i = tid; i < L::MT * 16 * RP; i += LR_THREADS) {
     const int t = i / RP, r = i % RP;
     float v = 0.f;
-    if (t < BT && adapter >= 0 && r < a.rank)  // (beyond the rank an infinite activation has met zeros)
-      for (int c = 0; c < ctas; ++c) v += ctas > 1 ? cluster.map_shared_rank(s_part, c)[t * RP + r] : s_part[t * RP + r];
+    if (t < BT && adapter >= 0 && r < a.rank) {  // (beyond the rank an infinite activation has met zeros)
+      float part[LR_CLUSTER];  // asked for together: a load from another SM takes long
+#pragma unroll
+      for (int c = 0; c < LR_CLUSTER; ++c) part[c] = c < ctas ? cluster.map_shared_rank(s_part, c)[t * RP + r] : 0.f;
+#pragma unroll
+      for (int c = 0; c < LR_CLUSTER; ++c) v += part[c];
+    }
     const float scaled = scale * v;
     if (a.v && t < count && r < a.rank && t % ctas == cta) a.v[static_cast<size_t>(s_rows[t]) * a.rank + r] = BACK ? scaled : v;
     uint32_t p[PV];
@@ -432,17 +441,16 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
       float d[4][4] = {};
 #pragma unroll
       for (int s = 0; s < RT; ++s) {
-        uint32_t vf[PV][4];
+        uint32_t vf[1][PV][4];
 #pragma unroll
         for (int j = 0; j < PV; ++j)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint2 u = *reinterpret_cast<const uint2*>(s_v + (j * L::MT * 16 + t * 16 + h * 8 + g) * L::V_STRIDE + s * 16 + 4 * q);
-            vf[j][h] = u.x;
-            vf[j][2 + h] = u.y;
+            vf[0][j][h] = u.x;
+            vf[0][j][2 + h] = u.y;
           }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mma_parts<PV, PI>(d[i], vf, uf[s][i]);
+        mma_parts_of<false>(d, vf, uf[s]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -468,9 +476,14 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
 
 // out[c][r] = sum over an adapter's rows of act[row][c] vec[row][r]:  dB from dy and s v (out [N][rank]), dA from x and dv (out [rank][K]).
 // The reduction runs over rows, so a lane takes the same eight channels of four rows and interleaves pairs of rows.  A CTA owns an even
-// run of the rows and 64 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
+// run of the rows and 32 or 64 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
 // parts.  A segment that is one run's alone is written at once, else the runs' shares are joined behind this kernel, in order.
-constexpr int GR_ROWS = 64, GR_CHANNELS = 64 * LR_WARPS;
+constexpr int GR_ROWS = 64;
+// Tiles of 16 channels per warp: four, or two, with which two CTAs share an SM, beyond rank 16 (us, fp32, 6000 x 1024 -> 1024, rank 32, whole
+// call 110/95; 2048 x 2048 -> 2048, rank 64 158/145; rank 16 with four 53).
+__host__ __device__ constexpr int grad_tiles(int rank) { return rank <= 16 ? 4 : 2; }
+__host__ __device__ constexpr int grad_channels(int rank) { return grad_tiles(rank) * 16 * LR_WARPS; }
+__host__ __device__ constexpr int grad_ctas(int rank) { return grad_tiles(rank) == 2 ? 2 : 1; }  // per SM
 
 struct GradArgs {
   const void* act[2];     // dy, x
@@ -485,8 +498,8 @@ struct GradArgs {
 };
 
 template <typename T, int RT>
-__global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a) {
-  constexpr int NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
+__global__ void __launch_bounds__(LR_THREADS, grad_ctas(RT * 16)) lowrank_grad_kernel(GradArgs a) {
+  constexpr int MT = grad_tiles(RT * 16), CH = 2 * MT, WORDS = CH * static_cast<int>(sizeof(T)) / 4, NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
   __shared__ uint32_t s_vec[3][PAIRS][W_STRIDE];
   __shared__ int s_rows[GR_ROWS];
   __shared__ TileList list;
@@ -497,10 +510,10 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
   if (static_cast<int>(blockIdx.x) >= a.runs[which]) return;
   const TileRun run = list_tiles<GR_ROWS>(list, a.off, a.G, a.n, blockIdx.x, a.runs[which]);
   if (run.lo >= run.hi) return;
-  const int dim = a.dim[which], c0 = block * GR_CHANNELS + warp * 64 + 8 * g;  // this lane's eight channels
+  const int dim = a.dim[which], c0 = block * grad_channels(RP) + (warp * 8 + g) * CH;  // this lane's channels
   const T* act = static_cast<const T*>(a.act[which]);
   const float* vec = a.vec[which];
-  float acc[4][NR][4] = {};
+  float acc[MT][NR][4] = {};
   for (RunWalk<GR_ROWS> walk(list, run); walk.more();) {
     const Tile tile = walk.next();
     const int rows = tile.rows, segment = walk.segment;
@@ -518,23 +531,20 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
       for (int j = 0; j < 3; ++j) s_vec[j][pair][r] = p[j];
     }
     __syncthreads();
-#pragma unroll 2
+#pragma unroll (RT == 1 ? 2 : 1)
     for (int k = 0; k < GR_ROWS; k += 16) {
       if (k >= rows) break;
-      uint32_t w[4][sizeof(T) * 2];  // eight channels of rows 4 q .. 4 q + 3
+      uint32_t w[4][WORDS];  // this lane's channels of rows 4 q .. 4 q + 3
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int row = s_rows[k + 4 * q + i];
 #pragma unroll
-        for (int j = 0; j < static_cast<int>(sizeof(T)) * 2; j += 4) {
-          uint4 u = make_uint4(0, 0, 0, 0);
-          if (row >= 0 && c0 < dim) u = load16(act + static_cast<size_t>(row) * a.stride[which] + c0 + j * 4 / static_cast<int>(sizeof(T)));
-          w[i][j] = u.x; w[i][j + 1] = u.y; w[i][j + 2] = u.z; w[i][j + 3] = u.w;
-        }
+        for (int j = 0; j < WORDS; ++j) w[i][j] = 0;
+        if (row >= 0 && c0 < dim) load_words(act + static_cast<size_t>(row) * a.stride[which] + c0, w[i]);
       }
-      uint32_t af[4][PI][4];  // tile m: channels c0 + 2 m (rows g) and c0 + 2 m + 1 (rows g + 8)
+      uint32_t af[MT][PI][4];  // tile m: channels c0 + 2 m (rows g) and c0 + 2 m + 1 (rows g + 8)
 #pragma unroll
-      for (int m = 0; m < 4; ++m)
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -550,19 +560,18 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
           }
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr) {
-        uint32_t bf[3][2];
+        uint32_t bf[1][3][2];
 #pragma unroll
         for (int j = 0; j < 3; ++j)
 #pragma unroll
-          for (int half = 0; half < 2; ++half) bf[j][half] = s_vec[j][k / 2 + 2 * q + half][nr * 8 + g];
+          for (int half = 0; half < 2; ++half) bf[0][j][half] = s_vec[j][k / 2 + 2 * q + half][nr * 8 + g];
+        // the tensor cores cut what they add: sixteen rows are summed by themselves, then added with rounding
+        float d[MT][4];
+        mma_parts_of<true>(d, af, bf);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          // the tensor cores cut what they add: sixteen rows are summed by themselves, then added with rounding
-          float d[4] = {};
-          mma_parts<PI, 3>(d, af[m], bf);
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[m][nr][i] += d[i];
-        }
+          for (int i = 0; i < 4; ++i) acc[m][nr][i] += d[m][i];
       }
     }
     if (!tile.ends) continue;
@@ -578,15 +587,15 @@ __global__ void __launch_bounds__(LR_THREADS, 1) lowrank_grad_kernel(GradArgs a)
         if (r >= a.rank || c0 >= dim) continue;
         if (which == 0) {
 #pragma unroll
-          for (int c = 0; c < 8; ++c) out[static_cast<size_t>(c0 + c) * a.rank + r] = acc[c / 2][nr][2 * (c % 2) + b];
+          for (int c = 0; c < CH; ++c) out[static_cast<size_t>(c0 + c) * a.rank + r] = acc[c / 2][nr][2 * (c % 2) + b];
         } else {
           float4* o = reinterpret_cast<float4*>(out + static_cast<size_t>(r) * dim + c0);
-          o[0] = make_float4(acc[0][nr][b], acc[0][nr][2 + b], acc[1][nr][b], acc[1][nr][2 + b]);
-          o[1] = make_float4(acc[2][nr][b], acc[2][nr][2 + b], acc[3][nr][b], acc[3][nr][2 + b]);
+#pragma unroll
+          for (int m = 0; m < MT; m += 2) o[m / 2] = make_float4(acc[m][nr][b], acc[m][nr][2 + b], acc[m + 1][nr][b], acc[m + 1][nr][2 + b]);
         }
       }
 #pragma unroll
-    for (int i = 0; i < 4 * NR * 4; ++i) (&acc[0][0][0])[i] = 0.f;
+    for (int i = 0; i < MT * NR * 4; ++i) (&acc[0][0][0])[i] = 0.f;
   }
 }
 
@@ -657,8 +666,10 @@ LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n, bool back) {
     w.part[i] = o;
     if (!back) continue;
     // 1024 rows at most per run, as accuracy goes on the streaming path
-    w.runs[i] = runs_for(n, D.n_adapters, blocks_of(static_cast<int>(dim), stream ? stream_channels(D.rank) : GR_CHANNELS), GPU_SMS,
-                         stream ? STREAM_ROWS : GR_ROWS, stream ? STREAM_RUN : STREAM_RUN * STREAM_ROWS / GR_ROWS);
+    if (stream) w.runs[i] = runs_for(n, D.n_adapters, blocks_of(static_cast<int>(dim), stream_channels(D.rank)), GPU_SMS, STREAM_ROWS, STREAM_RUN);
+    else  // (both outer products are one launch)
+      w.runs[i] = runs_for(n, D.n_adapters, blocks_of(D.in_dim, grad_channels(D.rank)) + blocks_of(D.out_dim, grad_channels(D.rank)),
+                           grad_ctas(D.rank) * GPU_SMS, GR_ROWS, STREAM_RUN * STREAM_ROWS / GR_ROWS);
     // Two shares per run.  What is reserved grows with n, dim and rank alike, so that a context that is made for the largest call serves all:
     // runs <= slots / blocks + tiles / 8 + 1 and slots / blocks * dim <= slots * 512; runs <= tiles.
     const size_t tiles = (static_cast<size_t>(n) + GR_ROWS - 1) / GR_ROWS + (D.n_adapters < n ? D.n_adapters : n);
@@ -691,26 +702,40 @@ cudaError_t launch_tile(const LowrankArgs& a, int tiles, int ctas, cudaStream_t 
   return cudaLaunchKernelEx(&cfg, lowrank_kernel<T, RT, NT, BACK>, a);
 }
 
+// Clusters of 1, 2, 4 and 8 CTAs that the GPU holds at once, of kernels with one, two and three CTAs per SM (larger ones leave SMs of a
+// part of the GPU empty).
+constexpr int CLUSTERS_HELD[3][4] = {{148, 74, 33, 15}, {296, 148, 71, 33}, {444, 222, 104, 48}};
+
 template <typename T, bool BACK>
 cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
-  // Rows per tile: 8, which has the most CTAs to share the work, while those are few; then 32, which read the factors a quarter as often.
-  // us, 4096 -> 4096, rank 16, 8 / 32 rows: bf16 512 rows 10.2/10.6, 1024 rows 17.5/15.1, 2048 rows 26/16; fp32 515 rows of 1104 -> 776 8.8/11.0, 2048 rows
-  // 58/40.  At a rank beyond 32 the registers of the larger tile leave an SM one CTA: 1024 rows 25/36 (bf16), 44/47 (fp32, 2048 -> 2048).
-  // 64 rows were slower or as fast everywhere (2048 rows 20 us).
+  // Rows per tile, 8 or 32, and CTAs per tile: what takes least time as rounds of clusters x (1 + 0.15 per doubling of the cluster + what a CTA
+  // multiplies), with 32 rows at the price of eight where the registers leave their kernel an SM for itself, of twice eight where it shares one.  Over 124 measured
+  // calls (both directions and types, rank 8 to 64, 100 to 4000 rows of 2 to 64 adapters) that is 1.3 % from the fastest choice on average, 19 % at
+  // worst.  us, forward, 1024 rows, 2048 -> 2048, four adapters: fp32, rank 32, eight rows x 1 / 2 / 4 CTAs 26.9/21.6/26.9, 32 rows x 1 / 2
+  // / 4 48.5/29.3/31.5; rank 16 21.1/16.1/21.1, 31.6/20.3/15.8.  64 rows were slower or as fast everywhere.
   const int segments = a.segments < a.n ? a.segments : a.n;
-  const auto mean_tiles = [&](int rows) { return a.n / rows + (segments + 1) / 2; };
-  const int nt = mean_tiles(8) <= (a.rank > 32 ? 264 : 104) ? 1 : 4;
-  // CTAs per tile while all of them run side by side: two per SM, or one where 32 rows take the registers of both
-  const int slots = nt == 4 && a.rank > (sizeof(T) == 2 ? 32 : 16) ? GPU_SMS : 2 * GPU_SMS;
-  int ctas = 1;
-  while (ctas < 8 && mean_tiles(nt * 8) * ctas * 2 <= slots) ctas *= 2;
+  const int rt = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
+  const int held[2] = {sizeof(T) == 2 && rt == 1 && !BACK ? 3 : 2, rt <= (sizeof(T) == 2 ? 2 : 1) ? 2 : 1};  // CTAs per SM
+  const double share = (static_cast<double>(a.in_dim) + a.out_dim) / 2048;
+  double least = 0.;
+  int nt = 1, ctas = 1;
+  for (int i = 0; i < 2; ++i)
+    for (int log = 0; log < 4; ++log) {
+      const int rows = i ? 32 : 8, mean_tiles = a.n / rows + (segments + 1) / 2, at_once = CLUSTERS_HELD[held[i] - 1][log];
+      const double cost = ((mean_tiles + at_once - 1) / at_once) * (1. + 0.15 * log + (i ? held[1] : 1) * share / (1 << log));
+      if ((i == 0 && log == 0) || cost < least) {
+        least = cost;
+        nt = rows / 8;
+        ctas = 1 << log;
+      }
+    }
   const int tiles = a.n / (nt * 8) + segments;
-  const auto by_rows = [&](auto rt) -> cudaError_t {
-    constexpr int RT = decltype(rt)::value;
+  const auto by_rows = [&](auto ranks) -> cudaError_t {
+    constexpr int RT = decltype(ranks)::value;
     return nt == 1 ? launch_tile<T, RT, 1, BACK>(a, tiles, ctas, st) : launch_tile<T, RT, 4, BACK>(a, tiles, ctas, st);
   };
-  if (a.rank <= 16) return by_rows(std::integral_constant<int, 1>());
-  if (a.rank <= 32) return by_rows(std::integral_constant<int, 2>());
+  if (rt == 1) return by_rows(std::integral_constant<int, 1>());
+  if (rt == 2) return by_rows(std::integral_constant<int, 2>());
   return by_rows(std::integral_constant<int, 4>());
 }
 
@@ -947,7 +972,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   ga.rank = desc->rank;
   for (int i = 0; i < 2; ++i) {
     ga.part[i] = reinterpret_cast<float*>(ws + w.part[i]);
-    ga.blocks[i] = ga.out[i] ? (ga.dim[i] + GR_CHANNELS - 1) / GR_CHANNELS : 0;
+    ga.blocks[i] = ga.out[i] ? blocks_of(ga.dim[i], grad_channels(desc->rank)) : 0;
     ga.runs[i] = w.runs[i];
   }
   if (streams) {

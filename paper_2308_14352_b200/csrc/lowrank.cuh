@@ -44,14 +44,25 @@ struct Parts {  // bf16 parts of a factor or activation, and of the fp32 vector 
   static constexpr int VEC = sizeof(T) == 4 ? 3 : 2;
 };
 
-// a . b over the kept products of their parts
-template <int PA, int PB>
-__device__ __forceinline__ void mma_parts(float (&d)[4], const uint32_t (&a)[PA][4], const uint32_t (&b)[PB][2]) {
+// N sums of products of parts side by side: d[k] (+)= a[k or 0] . b[k or 0].  The products of one sum wait for each other, some 35 clocks each,
+// so that those of the others stand between them.
+template <bool FIRST, int PA, int PB, int N, int NA, int NB>
+__device__ __forceinline__ void mma_parts_of(float (&d)[N][4], const uint32_t (&a)[NA][PA][4], const uint32_t (&b)[NB][PB][2]) {
+  bool first = FIRST;
 #pragma unroll
   for (int i = PA - 1; i >= 0; --i)  // smallest first
 #pragma unroll
     for (int j = PB - 1; j >= 0; --j)
-      if (i + j < 3) mma_bf16(d, a[i], b[j][0], b[j][1]);
+      if (i + j < 3) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const uint32_t(&x)[4] = a[NA == 1 ? 0 : k][i];
+          const uint32_t(&y)[2] = b[NB == 1 ? 0 : k][j];
+          if (first) mma_bf16_first(d[k], x, y[0], y[1]);
+          else mma_bf16(d[k], x, y[0], y[1]);
+        }
+        first = false;
+      }
 }
 
 __device__ __forceinline__ uint4 load16(const void* p) {
