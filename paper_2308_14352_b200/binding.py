@@ -1,4 +1,4 @@
-"""ctypes binding of libemoe.so: one Python function per C entry point of include/emoe.h,
+"""Python binding of libemoe.so: one Python function per C entry point of include/emoe.h,
 same names, argument marshalling only.  Tensors are passed as raw device pointers
 (``tensor.data_ptr()``), streams as ``torch.cuda.Stream.cuda_stream`` integers.
 
@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from types import SimpleNamespace
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -484,28 +485,54 @@ def emoe_rank_experts2(prior2_layer, prev2_ids, prev1_ids):
     return out
 
 
+# ---- rows in expert order, gates' gradient, low-rank adapters ----------------------------------
+# On small inputs these calls are shorter on the GPU than ctypes' own work per call, so they go through _pycall (csrc/pycall.cpp),
+# with the arguments' kinds from the declarations above.
+
+_fast = None
+
+
+def _calls() -> SimpleNamespace:
+    global _fast
+    if _fast is None:
+        L = lib()
+        try:
+            from . import _pycall
+        except ImportError as e:
+            raise RuntimeError("_pycall.so not found: build it with `python -m paper_2308_14352_b200.build`") from e
+        kind = {ctypes.c_void_p: "p", ctypes.c_int: "i"}
+        bound = {}
+        for name in ("emoe_dispatch", "emoe_dispatch_backward", "emoe_combine", "emoe_combine_backward", "emoe_gate_backward",
+                     "emoe_lowrank_forward", "emoe_lowrank_backward"):
+            f = getattr(L, name)
+            descs = tuple(t._type_ for t in f.argtypes if t not in kind)
+            bound[name] = _pycall.bind(ctypes.cast(f, ctypes.c_void_p).value, "".join(kind.get(t, "s") for t in f.argtypes), descs, L)
+        _fast = SimpleNamespace(**bound)
+    return _fast
+
+
 def emoe_dispatch(ctx, desc: emoe_dispatch_desc, x_ptr, T, ids_ptr, weights_ptr, counts_ptr, off_ptr, perm_ptr, slot_of_pair_ptr, rows_ptr,
                   stream=0) -> None:
-    _check(lib().emoe_dispatch(ctx, desc, x_ptr, T, ids_ptr, weights_ptr, counts_ptr, off_ptr, perm_ptr, slot_of_pair_ptr, rows_ptr, stream),
+    _check(_calls().emoe_dispatch(ctx, desc, x_ptr, T, ids_ptr, weights_ptr, counts_ptr, off_ptr, perm_ptr, slot_of_pair_ptr, rows_ptr, stream),
            "emoe_dispatch")
 
 
 def emoe_dispatch_backward(ctx, desc: emoe_dispatch_desc, drows_ptr, T, slot_of_pair_ptr, weights_ptr, x_ptr, dx_ptr, dweights_ptr, stream=0) -> None:
-    _check(lib().emoe_dispatch_backward(ctx, desc, drows_ptr, T, slot_of_pair_ptr, weights_ptr, x_ptr, dx_ptr, dweights_ptr, stream),
+    _check(_calls().emoe_dispatch_backward(ctx, desc, drows_ptr, T, slot_of_pair_ptr, weights_ptr, x_ptr, dx_ptr, dweights_ptr, stream),
            "emoe_dispatch_backward")
 
 
 def emoe_combine(ctx, desc: emoe_dispatch_desc, rows_ptr, T, slot_of_pair_ptr, gates_ptr, y_ptr, stream=0) -> None:
-    _check(lib().emoe_combine(ctx, desc, rows_ptr, T, slot_of_pair_ptr, gates_ptr, y_ptr, stream), "emoe_combine")
+    _check(_calls().emoe_combine(ctx, desc, rows_ptr, T, slot_of_pair_ptr, gates_ptr, y_ptr, stream), "emoe_combine")
 
 
 def emoe_combine_backward(ctx, desc: emoe_dispatch_desc, dy_ptr, T, slot_of_pair_ptr, gates_ptr, rows_ptr, drows_ptr, dgates_ptr, stream=0) -> None:
-    _check(lib().emoe_combine_backward(ctx, desc, dy_ptr, T, slot_of_pair_ptr, gates_ptr, rows_ptr, drows_ptr, dgates_ptr, stream),
+    _check(_calls().emoe_combine_backward(ctx, desc, dy_ptr, T, slot_of_pair_ptr, gates_ptr, rows_ptr, drows_ptr, dgates_ptr, stream),
            "emoe_combine_backward")
 
 
 def emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream=0) -> None:
-    _check(lib().emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream), "emoe_gate_backward")
+    _check(_calls().emoe_gate_backward(ctx, logits_ptr, T, E, ids_ptr, dgates_ptr, top_k, gate_mode, dlogits_ptr, stream), "emoe_gate_backward")
 
 
 def emoe_lowrank_workspace_bytes(desc: emoe_lowrank_desc, n: int) -> int:
@@ -514,11 +541,11 @@ def emoe_lowrank_workspace_bytes(desc: emoe_lowrank_desc, n: int) -> int:
 
 def emoe_lowrank_forward(ctx, desc: emoe_lowrank_desc, A_ptr, B_ptr, scales_ptr, x_ptr, n, ids_ptr, off_ptr, base_ptr, y_ptr, out_v_ptr,
                          stream=0) -> None:
-    _check(lib().emoe_lowrank_forward(ctx, desc, A_ptr, B_ptr, scales_ptr, x_ptr, n, ids_ptr, off_ptr, base_ptr, y_ptr, out_v_ptr, stream),
+    _check(_calls().emoe_lowrank_forward(ctx, desc, A_ptr, B_ptr, scales_ptr, x_ptr, n, ids_ptr, off_ptr, base_ptr, y_ptr, out_v_ptr, stream),
            "emoe_lowrank_forward")
 
 
 def emoe_lowrank_backward(ctx, desc: emoe_lowrank_desc, A_ptr, B_ptr, scales_ptr, x_ptr, dy_ptr, n, ids_ptr, off_ptr, v_ptr, dx_base_ptr, dx_ptr,
                           dA_ptr, dB_ptr, stream=0) -> None:
-    _check(lib().emoe_lowrank_backward(ctx, desc, A_ptr, B_ptr, scales_ptr, x_ptr, dy_ptr, n, ids_ptr, off_ptr, v_ptr, dx_base_ptr, dx_ptr,
+    _check(_calls().emoe_lowrank_backward(ctx, desc, A_ptr, B_ptr, scales_ptr, x_ptr, dy_ptr, n, ids_ptr, off_ptr, v_ptr, dx_base_ptr, dx_ptr,
                                        dA_ptr, dB_ptr, stream), "emoe_lowrank_backward")
