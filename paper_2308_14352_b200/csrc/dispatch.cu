@@ -606,9 +606,34 @@ cudaError_t by_types(int row_dtype, int token_dtype, Width width, F&& f) {
   return tb ? by_width(Tag<float>(), Tag<__nv_bfloat16>()) : by_width(Tag<float>(), Tag<float>());
 }
 
-int threads_per_token(int d, int vec) {
-  const int pieces = (d + vec - 1) / vec;
-  return pieces <= 32 ? 32 : pieces <= 64 ? 64 : pieces <= 128 ? 128 : 256;
+// Threads of a token, by the pieces of its row.  Wide pieces: as few as take the row in one `round` of pieces asked for together, while that
+// leaves work for 64 K threads, and as leave each `most` times 16 bytes (of the wider type), while that fills the SMs (`ctas` each): rows in flight hide more
+// than threads on one row.  us, a thread per piece / as ruled: combine 8192 x 1024, one pick 9.7/5.8, 8192 x 2048, two picks 24.5/18.1; its gradient,
+// 30000 x 512, one pick 28.4/19.4; 1100 x 1024, two picks 2.9/2.2 (32 threads 2.8); 300 x 1024, eight picks 2.8 with 128 threads, 5.0 with
+// 32.  Narrower pieces: about a thread per 16 bytes (combine 8192 x 1101, two picks, 32 / 64 / 128 / 256 threads 30.7/25.5/26.4/31.3; 4000 x 777,
+// eight picks 34.5/37.0/31.5/35.1).  Over 92 calls 12 % less than a thread per piece, 2 % more than the best.
+int threads_per_token(const emoe_dispatch_desc& D, int T, Width width, int round, int most, int ctas) {
+  const size_t size = D.row_dtype == EMOE_DTYPE_BF16 && D.token_dtype == EMOE_DTYPE_BF16 ? 2 : 4;
+  const long long words = static_cast<long long>((D.d * size + 15) / 16), pieces = D.row_dtype == EMOE_DTYPE_BF16 ? (D.d + 7) / 8 : (D.d + 3) / 4;
+  int t = 32;
+  if (width != WIDE) {
+    while (t < ROWS_THREADS && 2LL * t * t < words * words) t *= 2;
+    return t;
+  }
+  while (t < ROWS_THREADS && t < pieces) t *= 2;
+  const auto halves = [&](int each, long long of, long long threads) {
+    return t > 32 && static_cast<long long>(t / 2) * each >= of && static_cast<long long>(T) * (t / 2) >= threads;
+  };
+  while (halves(round, pieces, 1 << 16) || halves(most, words, static_cast<long long>(ctas) * ROWS_THREADS * GPU_SMS)) t /= 2;
+  return t;
+}
+int gather_threads(const emoe_dispatch_desc& D, const RowsArgs& a, Width width) {
+  const int picks = a.top_k <= 2 ? (a.dots ? 2 : a.top_k) : a.top_k <= 4 && !a.dots ? 4 : 8;
+  return threads_per_token(D, a.T, width, picks > 2 ? 1 : picks == 1 ? 4 : 2, 4, gather_ctas(picks, a.dots));
+}
+// (a spread writes top_k rows per piece: 4000 x 2048, eight picks, two / four pieces 30.8/35.0, with products 47.1/49.7)
+int spread_threads(const emoe_dispatch_desc& D, const RowsArgs& a, Width width) {
+  return threads_per_token(D, a.T, width, a.dots && a.top_k > 2 ? 1 : 2, a.dots && a.top_k <= 2 ? 4 : 2, spread_ctas(a.top_k <= 2 ? 2 : 8, a.dots));
 }
 
 Width width_of(const emoe_dispatch_desc& D, const RowsArgs& a, const void* rows, const void* rows_too, const void* tokens, const void* tokens_too) {
@@ -627,7 +652,7 @@ cudaError_t launch_gather(const emoe_dispatch_desc& D, RowsArgs a, cudaStream_t 
     using RowT = typename decltype(row)::type;
     using TokT = typename decltype(tok)::type;
     constexpr int VEC = decltype(vec)::value;
-    a.threads_per_token = threads_per_token(a.d, VEC);
+    a.threads_per_token = gather_threads(D, a, wide);
     const int per_cta = ROWS_THREADS / a.threads_per_token;
     const auto go = [&](auto kernel) { return launch_chain(kernel, dim3((a.T + per_cta - 1) / per_cta), dim3(ROWS_THREADS), 0, st, a); };
     if (a.dots) return a.top_k <= 2 ? go(gather_kernel<RowT, TokT, VEC, 2, true>) : go(gather_kernel<RowT, TokT, VEC, 8, true>);
@@ -644,7 +669,7 @@ cudaError_t launch_spread(const emoe_dispatch_desc& D, RowsArgs a, cudaStream_t 
     using RowT = typename decltype(row)::type;
     using TokT = typename decltype(tok)::type;
     constexpr int VEC = decltype(vec)::value;
-    a.threads_per_token = threads_per_token(a.d, VEC);
+    a.threads_per_token = spread_threads(D, a, wide);
     const int per_cta = ROWS_THREADS / a.threads_per_token;
     const auto go = [&](auto kernel) { return launch_chain(kernel, dim3((a.T + per_cta - 1) / per_cta), dim3(ROWS_THREADS), 0, st, a); };
     if (a.dots) return a.top_k <= 2 ? go(spread_kernel<RowT, TokT, VEC, 2, true>) : go(spread_kernel<RowT, TokT, VEC, 8, true>);
@@ -759,7 +784,8 @@ int emoe_dispatch(emoe_ctx* ctx, const emoe_dispatch_desc* desc, const void* x, 
   const size_t z = dtype_size(desc->token_dtype), bytes = desc->d * z;
   if (bytes % 16 == 0 && a.token_stride * z % 16 == 0 && ptr_aligned(x, 16) && bytes <= (1 << 20)) {
     // some 32 MB, a quarter of L2
-    const size_t round = bytes * SPREAD_FIRST * (ROWS_THREADS / threads_per_token(desc->d, desc->row_dtype == EMOE_DTYPE_BF16 ? 8 : 4)), rounds = (32u << 20) / round;
+    const int threads = spread_threads(*desc, a, width_of(*desc, a, a.out, nullptr, a.in, nullptr));
+    const size_t round = bytes * SPREAD_FIRST * (ROWS_THREADS / threads), rounds = (32u << 20) / round;
     a.ahead = rounds < 1 ? 1 : rounds < 16 ? static_cast<int>(rounds) : 16;
     a.ahead_bytes = static_cast<int>(bytes);
   }
