@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(ROWS_THREADS)
   }
   const int t = blockIdx.x;
   const TokT* x = static_cast<const TokT*>(a.in) + static_cast<size_t>(t) * a.token_stride;
-  constexpr int U = 2;
+  constexpr int U = VEC <= 2 ? 8 : 2;  // pieces asked for together (narrow ones, two / eight: 2000 x 5001, one pick 27/22, 60 x 1101, two picks 2.4/1.9)
   Piece<TokT, VEC> px[U];
 #pragma unroll
   for (int u = 0; u < U; ++u)
