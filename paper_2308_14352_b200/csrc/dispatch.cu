@@ -629,7 +629,8 @@ int threads_per_token(const emoe_dispatch_desc& D, int T, Width width, int round
 }
 int gather_threads(const emoe_dispatch_desc& D, const RowsArgs& a, Width width) {
   const int picks = a.top_k <= 2 ? (a.dots ? 2 : a.top_k) : a.top_k <= 4 && !a.dots ? 4 : 8;
-  return threads_per_token(D, a.T, width, picks > 2 ? 1 : picks == 1 ? 4 : 2, 4, gather_ctas(picks, a.dots));
+  const bool widens = D.row_dtype == EMOE_DTYPE_BF16 && D.token_dtype == EMOE_DTYPE_F32;  // (2048 x 1024, one pick, 32 / 64 / 128 threads 4.3/4.8/3.6 us)
+  return threads_per_token(D, a.T, width, picks > 2 || (picks == 1 && widens) ? 1 : picks == 1 ? 4 : 2, 4, gather_ctas(picks, a.dots));
 }
 // (a spread writes top_k rows per piece: 4000 x 2048, eight picks, two / four pieces 30.8/35.0, with products 47.1/49.7)
 int spread_threads(const emoe_dispatch_desc& D, const RowsArgs& a, Width width) {
