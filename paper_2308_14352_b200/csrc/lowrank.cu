@@ -476,14 +476,11 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
 
 // out[c][r] = sum over an adapter's rows of act[row][c] vec[row][r]:  dB from dy and s v (out [N][rank]), dA from x and dv (out [rank][K]).
 // The reduction runs over rows, so a lane takes the same eight channels of four rows and interleaves pairs of rows.  A CTA owns an even
-// run of the rows and 32 or 64 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
+// run of the rows and 32 channels per warp; the vectors of 64 rows at a time lie in shared memory as pairs of rows in three bf16
 // parts.  A segment that is one run's alone is written at once, else the runs' shares are joined behind this kernel, in order.
-constexpr int GR_ROWS = 64;
-// Tiles of 16 channels per warp: four, or two, with which two CTAs share an SM, beyond rank 16 (us, fp32, 6000 x 1024 -> 1024, rank 32, whole
-// call 110/95; 2048 x 2048 -> 2048, rank 64 158/145; rank 16 with four 53).
-__host__ __device__ constexpr int grad_tiles(int rank) { return rank <= 16 ? 4 : 2; }
-__host__ __device__ constexpr int grad_channels(int rank) { return grad_tiles(rank) * 16 * LR_WARPS; }
-__host__ __device__ constexpr int grad_ctas(int rank) { return grad_tiles(rank) == 2 ? 2 : 1; }  // per SM
+// Two tiles of 16 channels per warp leave two CTAs an SM; with four a CTA has one for itself and, beyond rank 16, too few registers (us, whole
+// call, fp32, four / two: 1561 x 4864 -> 3360, rank 16 75/72; 6000 x 1024 -> 1024, rank 32 110/95; 2048 x 2048 -> 2048, rank 64 158/145).
+constexpr int GR_ROWS = 64, GR_TILES = 2, GR_CHANNELS = GR_TILES * 16 * LR_WARPS, GR_CTAS = 2;
 
 struct GradArgs {
   const void* act[2];     // dy, x
@@ -498,8 +495,8 @@ struct GradArgs {
 };
 
 template <typename T, int RT>
-__global__ void __launch_bounds__(LR_THREADS, grad_ctas(RT * 16)) lowrank_grad_kernel(GradArgs a) {
-  constexpr int MT = grad_tiles(RT * 16), CH = 2 * MT, WORDS = CH * static_cast<int>(sizeof(T)) / 4, NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
+__global__ void __launch_bounds__(LR_THREADS, GR_CTAS) lowrank_grad_kernel(GradArgs a) {
+  constexpr int MT = GR_TILES, CH = 2 * MT, WORDS = CH * static_cast<int>(sizeof(T)) / 4, NR = RT * 2, RP = RT * 16, PI = Parts<T>::IN, PAIRS = GR_ROWS / 2, W_STRIDE = RP + 4;
   __shared__ uint32_t s_vec[3][PAIRS][W_STRIDE];
   __shared__ int s_rows[GR_ROWS];
   __shared__ TileList list;
@@ -510,7 +507,7 @@ __global__ void __launch_bounds__(LR_THREADS, grad_ctas(RT * 16)) lowrank_grad_k
   if (static_cast<int>(blockIdx.x) >= a.runs[which]) return;
   const TileRun run = list_tiles<GR_ROWS>(list, a.off, a.G, a.n, blockIdx.x, a.runs[which]);
   if (run.lo >= run.hi) return;
-  const int dim = a.dim[which], c0 = block * grad_channels(RP) + (warp * 8 + g) * CH;  // this lane's channels
+  const int dim = a.dim[which], c0 = block * GR_CHANNELS + (warp * 8 + g) * CH;  // this lane's channels
   const T* act = static_cast<const T*>(a.act[which]);
   const float* vec = a.vec[which];
   float acc[MT][NR][4] = {};
@@ -668,8 +665,8 @@ LowrankLayout lowrank_layout(const emoe_lowrank_desc& D, int n, bool back) {
     // 1024 rows at most per run, as accuracy goes on the streaming path
     if (stream) w.runs[i] = runs_for(n, D.n_adapters, blocks_of(static_cast<int>(dim), stream_channels(D.rank)), GPU_SMS, STREAM_ROWS, STREAM_RUN);
     else  // (both outer products are one launch)
-      w.runs[i] = runs_for(n, D.n_adapters, blocks_of(D.in_dim, grad_channels(D.rank)) + blocks_of(D.out_dim, grad_channels(D.rank)),
-                           grad_ctas(D.rank) * GPU_SMS, GR_ROWS, STREAM_RUN * STREAM_ROWS / GR_ROWS);
+      w.runs[i] = runs_for(n, D.n_adapters, blocks_of(D.in_dim, GR_CHANNELS) + blocks_of(D.out_dim, GR_CHANNELS),
+                           GR_CTAS * GPU_SMS, GR_ROWS, STREAM_RUN * STREAM_ROWS / GR_ROWS);
     // Two shares per run.  What is reserved grows with n, dim and rank alike, so that a context that is made for the largest call serves all:
     // runs <= slots / blocks + tiles / 8 + 1 and slots / blocks * dim <= slots * 512; runs <= tiles.
     const size_t tiles = (static_cast<size_t>(n) + GR_ROWS - 1) / GR_ROWS + (D.n_adapters < n ? D.n_adapters : n);
@@ -741,7 +738,9 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
 
 cudaError_t launch_join(const GradArgs& a, bool stream, cudaStream_t st) {
   const size_t dim = a.dim[0] > a.dim[1] ? a.dim[0] : a.dim[1], shares = (dim * a.rank / 4 + LR_THREADS - 1) / LR_THREADS;
-  const dim3 grid(a.G, static_cast<unsigned>(shares < 32 ? shares : 32), 2);
+  // CTAs of an adapter's gradient: few adapters share all SMs (8192 x 4096 -> 4096, one adapter, whole call 77/71 us)
+  const size_t most = 2 * GPU_SMS / a.G > 32 ? 2 * GPU_SMS / a.G : 32;
+  const dim3 grid(a.G, static_cast<unsigned>(shares < most ? shares : most), 2);
   if (stream) return launch_chain(lowrank_join_kernel<STREAM_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
   return launch_chain(lowrank_join_kernel<GR_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
 }
@@ -972,7 +971,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   ga.rank = desc->rank;
   for (int i = 0; i < 2; ++i) {
     ga.part[i] = reinterpret_cast<float*>(ws + w.part[i]);
-    ga.blocks[i] = ga.out[i] ? blocks_of(ga.dim[i], grad_channels(desc->rank)) : 0;
+    ga.blocks[i] = ga.out[i] ? blocks_of(ga.dim[i], GR_CHANNELS) : 0;
     ga.runs[i] = w.runs[i];
   }
   if (streams) {
