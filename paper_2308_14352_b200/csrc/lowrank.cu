@@ -33,6 +33,7 @@ struct LowrankArgs {
   void* y;               // null: the low-rank vectors alone
   float* v;              // null: not wanted
   int* check_word;
+  int32_t *off_out, *perm_out;  // given: one tile more writes the order of the ids there, for the kernels behind
   int n, G, rank, in_dim, out_dim, segments;  // segments: G, or G + 1 with the rows of no adapter as the last
   int skip_none;         // rows of no adapter stay as they are
   size_t x_stride, y_stride;
@@ -128,6 +129,75 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
   return count;
 }
 
+// The order of at most LR_IDS_ROWS ids as launch_sort_pairs writes it (ids of no adapter behind the others), by one CTA beside those that multiply: a
+// launch in front of them takes some 4 us (backward, bf16, 64 rows of 8 adapters, 2048 -> 2048, 16.0/12.2; 1000 of 60, 512 -> 512, 19.8/14.9).  A warp owns consecutive rows: it counts them by adapter, then hands out their places.
+__device__ __forceinline__ void write_order(const LowrankArgs& a, int (*first)[EMOE_MAX_EXPERTS + 1], int* s_scan) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, segments = a.G + 1, bits = 32 - __clz(a.G);
+  constexpr int STEPS = LR_IDS_ROWS / LR_THREADS;
+  for (int i = tid; i < LR_WARPS * segments; i += LR_THREADS) first[i / segments][i % segments] = 0;
+  __syncthreads();
+  int id[STEPS], front[STEPS];
+  unsigned same[STEPS];
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int row = (warp * STEPS + i) * 32 + lane;
+    id[i] = row < a.n ? a.ids[row] : -2;
+    if (row < a.n && (id[i] < 0 || id[i] >= a.G)) id[i] = a.G;
+  }
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    same[i] = __ballot_sync(0xffffffffu, id[i] >= 0);
+    for (int b = 0; b < bits; ++b) {
+      const unsigned set = __ballot_sync(0xffffffffu, id[i] >> b & 1);
+      same[i] &= (id[i] >> b & 1) ? set : ~set;
+    }
+    front[i] = __popc(same[i] & ((1u << lane) - 1u));
+    if (id[i] >= 0 && front[i] == 0) first[warp][id[i]] += __popc(same[i]);
+    __syncwarp();
+  }
+  __syncthreads();
+  const auto rows_of = [&](int e) {
+    int sum = 0;
+    for (int w = 0; w < LR_WARPS; ++w) sum += first[w][e];
+    return sum;
+  };
+  const int rows = tid < segments ? rows_of(tid) : 0;
+  int incl = rows;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) s_scan[warp] = incl;
+  __syncthreads();
+  int before = incl - rows, all = 0;
+  for (int w = 0; w < LR_WARPS; ++w) {
+    if (w < warp) before += s_scan[w];
+    all += s_scan[w];
+  }
+  const auto hand_out = [&](int e, int at) {
+    a.off_out[e] = at;
+    for (int w = 0; w < LR_WARPS; ++w) {
+      const int c = first[w][e];
+      first[w][e] = at;
+      at += c;
+    }
+  };
+  if (tid < segments) hand_out(tid, before);
+  if (tid == 0) {
+    if (segments > LR_THREADS) hand_out(LR_THREADS, all);  // a 257th segment
+    a.off_out[segments] = a.n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    if (id[i] >= 0) a.perm_out[first[warp][id[i]] + front[i]] = (warp * STEPS + i) * 32 + lane;
+    __syncwarp();
+    if (id[i] >= 0 && front[i] == 0) first[warp][id[i]] += __popc(same[i]);
+    __syncwarp();
+  }
+}
+
 // RT: rank in tiles of 16; NT: rows in tiles of 8; BACK: the down factor is B ([reduction][rank]), the up factor A ([rank][out]).
 template <typename T, int RT, int NT, bool BACK>
 struct Lowrank {
@@ -191,6 +261,13 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
   const int ctas = static_cast<int>(cluster.num_blocks()), cta = static_cast<int>(cluster.block_rank());
   pdl_wait();
   pdl_trigger();
+  if constexpr (BACK) {
+    __shared__ int first[LR_WARPS][EMOE_MAX_EXPERTS + 1];
+    if (a.perm_out && blockIdx.x / ctas == gridDim.x / ctas - 1) {
+      if (cta == 0) write_order(a, first, s_scan);
+      return;
+    }
+  }
   int adapter = -1;
   const int count = find_rows<BT>(a, blockIdx.x / ctas, s_rows, s_scan, s_count, &adapter);
   if (count == 0 || (adapter < 0 && a.skip_none && !a.v)) return;  // the whole cluster
@@ -726,7 +803,7 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
         ctas = 1 << log;
       }
     }
-  const int tiles = a.n / (nt * 8) + segments;
+  const int tiles = a.n / (nt * 8) + segments + (a.perm_out ? 1 : 0);
   const auto by_rows = [&](auto ranks) -> cudaError_t {
     constexpr int RT = decltype(ranks)::value;
     return nt == 1 ? launch_tile<T, RT, 1, BACK>(a, tiles, ctas, st) : launch_tile<T, RT, 4, BACK>(a, tiles, ctas, st);
@@ -947,10 +1024,16 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   a.y_stride = static_cast<size_t>(desc->x_stride ? desc->x_stride : desc->in_dim);
   a.off = off;
   if (ids) {
-    EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, true, nullptr, a.check_word, st));
-    a.off = off_ws;
-    a.perm = perm;
     a.segments = desc->n_adapters + 1;
+    if (n <= LR_IDS_ROWS && !streams && (dx || dA)) {
+      a.ids = ids;
+      a.off_out = off_ws;
+      a.perm_out = perm;
+    } else {
+      EMOE_CALL(ctx, launch_sort_pairs(ids, n, desc->n_adapters + 1, true, nullptr, off_ws, perm, true, nullptr, a.check_word, st));
+      a.off = off_ws;
+      a.perm = perm;
+    }
   }
   GradArgs ga = {};
   ga.act[0] = dy;
@@ -964,8 +1047,8 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   ga.out[0] = dB;
   ga.out[1] = dA;
   ga.scales = scales;
-  ga.off = a.off;
-  ga.perm = a.perm;
+  ga.off = ids ? off_ws : off;
+  ga.perm = ids ? perm : nullptr;
   ga.n = n;
   ga.G = desc->n_adapters;
   ga.rank = desc->rank;
