@@ -64,12 +64,10 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
     __syncthreads();
   }
   // one thread per segment: its tiles, added up
-  int begin = 0, rows = 0;
-  if (tid < a.segments) {
-    begin = a.ids ? 0 : min(max(a.off[tid], 0), a.n);
-    rows = a.ids ? s_count[tid] : min(a.off[tid + 1], a.n) - begin;
-  }
-  const int tiles = rows > 0 ? (rows + BT - 1) / BT : 0;
+  const auto span = [&](int i) { return a.ids ? RowSpan{0, s_count[i]} : span_of(a.off, i, a.n); };
+  RowSpan mine = {0, 0};
+  if (tid < a.segments) mine = span(tid);
+  const int tiles = (mine.rows + BT - 1) / BT;
   int incl = tiles;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -79,11 +77,8 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
   if (lane == 31) s_scan[warp] = incl;
   if (tid == 0) s_scan[LR_WARPS] = 0;
   // (a 257th segment, the rows of no adapter beside 256 of them)
-  int last_begin = 0, last_rows = 0;
-  if (a.segments > LR_THREADS) {
-    last_begin = a.ids ? 0 : min(max(a.off[LR_THREADS], 0), a.n);
-    last_rows = a.ids ? s_count[LR_THREADS] : min(a.off[LR_THREADS + 1], a.n) - last_begin;
-  }
+  RowSpan last = {0, 0};
+  if (a.segments > LR_THREADS) last = span(LR_THREADS);
   __syncthreads();
   int front = 0, all = 0;
   for (int w = 0; w < LR_WARPS; ++w) {
@@ -92,13 +87,13 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
   }
   const int first = front + incl - tiles;
   if (tile >= first && tile < first + tiles) {
-    s_scan[LR_WARPS] = min(BT, rows - (tile - first) * BT);
-    s_scan[LR_WARPS + 1] = begin + (tile - first) * BT;
+    s_scan[LR_WARPS] = min(BT, mine.rows - (tile - first) * BT);
+    s_scan[LR_WARPS + 1] = mine.begin + (tile - first) * BT;
     s_scan[LR_WARPS + 2] = tid;
   }
-  if (tid == 0 && last_rows > 0 && tile >= all && tile < all + (last_rows + BT - 1) / BT) {
-    s_scan[LR_WARPS] = min(BT, last_rows - (tile - all) * BT);
-    s_scan[LR_WARPS + 1] = last_begin + (tile - all) * BT;
+  if (tid == 0 && tile >= all && tile < all + (last.rows + BT - 1) / BT) {
+    s_scan[LR_WARPS] = min(BT, last.rows - (tile - all) * BT);
+    s_scan[LR_WARPS + 1] = last.begin + (tile - all) * BT;
     s_scan[LR_WARPS + 2] = LR_THREADS;
   }
   __syncthreads();

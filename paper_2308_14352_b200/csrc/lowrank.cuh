@@ -72,6 +72,16 @@ __device__ __forceinline__ uint4 load16(const void* p) {
 }
 __device__ __forceinline__ uint4 load16_keep(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
+// The rows of segment i, off[i] .. off[i + 1] - 1, as far as there are such rows: the offsets are the caller's, and whatever they hold, both ends are
+// cut to the rows before they are subtracted.
+struct RowSpan {
+  int begin, rows;
+};
+__device__ __forceinline__ RowSpan span_of(const int32_t* __restrict__ off, int i, int n) {
+  const int begin = min(max(off[i], 0), n), end = min(max(off[i + 1], 0), n);
+  return {begin, max(end - begin, 0)};
+}
+
 // ---- rows shared out evenly ----------------------------------------------------------------------
 // The rows of every segment (the G adapters and, where there is one more, the rows of none) make tiles of H rows, the last of a
 // segment with fewer; the tiles of all segments, one behind the other, are cut into even runs, one per CTA.  A run may begin and end
@@ -93,10 +103,10 @@ template <int H>
 __device__ __forceinline__ TileRun list_tiles(TileList& list, const int32_t* __restrict__ off, int segments, int n, int cta, int ctas) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const auto segment = [&](int i) {
-    const int begin = min(max(off[i], 0), n), rows = max(min(off[i + 1], n) - begin, 0);
-    list.begin[i] = begin;
-    list.rows[i] = rows;
-    return (rows + H - 1) / H;
+    const RowSpan span = span_of(off, i, n);
+    list.begin[i] = span.begin;
+    list.rows[i] = span.rows;
+    return (span.rows + H - 1) / H;
   };
   const int tiles = tid < min(segments, LR_THREADS) ? segment(tid) : 0;
   int last = 0;
