@@ -514,7 +514,7 @@ __global__ void __launch_bounds__(256)
     const float sum = group_sum(g);
     g = sum != 0.f ? g / sum : 0.f;
     const float c = group_sum(pick >= 0 ? g * dg : 0.f);
-    const float dz = g * (dg - c);
+    const float dz = sum != 0.f ? g * (dg - c) : 0.f;  // (no logit left: zero, whatever dg is)
 #pragma unroll
     for (int i = 0; i < V; ++i) out[i] = 0.f;
     for (int j = 0; j < top_k; ++j) {
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(256)
     }
     c = group_sum(c);
 #pragma unroll
-    for (int i = 0; i < V; ++i) out[i] = p[i] * (out[i] - c);
+    for (int i = 0; i < V; ++i) out[i] = sum != 0.f ? p[i] * (out[i] - c) : 0.f;
   }
   if (!live) return;
   float* dz = dlogits + static_cast<size_t>(t) * E;
