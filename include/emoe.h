@@ -261,8 +261,8 @@ int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const i
  * Sums are fp32 or better; bf16 results are rounded once, fp32 tensors are multiplied with all their 24 bits; the same inputs give the same
  * bits.  Infinities: bf16 rows give what the formulas give; an infinite value of an fp32 tensor or of a factor, and in dA and dB of
  * any, may give NaN where they give an infinity.
- * Limits: rank 1 .. EMOE_MAX_RANK (any; multiples of 8 are faster), in_dim and out_dim multiples of 8, strides multiples of 16 bytes, tensors
- * 16-byte aligned, n < 2^27. */
+ * Limits: rank 1 .. EMOE_MAX_RANK (any; multiples of 8 are faster), in_dim and out_dim multiples of 8 and at most 8388352, strides multiples of
+ * 16 bytes, tensors 16-byte aligned, n < 2^27. */
 typedef struct emoe_lowrank_desc {
   int32_t n_adapters; /* 1 .. EMOE_MAX_EXPERTS */
   int32_t rank;

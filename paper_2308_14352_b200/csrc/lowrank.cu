@@ -553,6 +553,7 @@ __global__ void __launch_bounds__(LR_THREADS, NT == 1 || RT <= (sizeof(T) == 2 ?
 // Two tiles of 16 channels per warp leave two CTAs an SM; with four a CTA has one for itself and, beyond rank 16, too few registers (us, whole
 // call, fp32, four / two: 1561 x 4864 -> 3360, rank 16 75/72; 6000 x 1024 -> 1024, rank 32 110/95; 2048 x 2048 -> 2048, rank 64 158/145).
 constexpr int GR_ROWS = 64, GR_TILES = 2, GR_CHANNELS = GR_TILES * 16 * LR_WARPS, GR_CTAS = 2;
+constexpr int LR_MAX_DIM = 65535 / 2 * GR_CHANNELS;  // the blocks of dB and dA stand side by side in one grid, 65535 high at most
 
 struct GradArgs {
   const void* act[2];     // dy, x
@@ -899,7 +900,7 @@ int check_lowrank(const emoe_lowrank_desc* D, int n, const int32_t* ids, const i
   if ((ids == nullptr) == (off == nullptr)) return EMOE_ERR_INVALID_ARG;
   if ((D->x_stride && D->x_stride < D->in_dim) || (D->y_stride && D->y_stride < D->out_dim)) return EMOE_ERR_INVALID_ARG;
   if (!dtype_ok(D->dtype) || D->rank > EMOE_MAX_RANK) return EMOE_ERR_UNSUPPORTED;
-  if (D->in_dim % 8 != 0 || D->out_dim % 8 != 0 || D->in_dim > 0x7fffffff / 256 || D->out_dim > 0x7fffffff / 256) return EMOE_ERR_UNSUPPORTED;
+  if (D->in_dim % 8 != 0 || D->out_dim % 8 != 0 || D->in_dim > LR_MAX_DIM || D->out_dim > LR_MAX_DIM) return EMOE_ERR_UNSUPPORTED;
   if (n > 0x7fffffff / 16) return EMOE_ERR_UNSUPPORTED;
   const int64_t vec = 16 / static_cast<int64_t>(dtype_size(D->dtype));
   if (D->x_stride % vec != 0 || D->y_stride % vec != 0) return EMOE_ERR_ALIGNMENT;
