@@ -258,6 +258,7 @@ int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const i
  * one of the two is given.
  * Rows of no adapter: with ids y = base and v = 0 (nothing is touched where y is base), with off they are left as they were; they
  * take no part in dA and dB.  An id other than -1 outside [0,n_adapters) counts as -1 and sets the device check word.
+ * Offsets that descend or lie outside 0 .. n set it too; the results of such a call are undefined, but nothing outside its tensors is touched.
  * Sums are fp32 or better; bf16 results are rounded once, fp32 tensors are multiplied with all their 24 bits; the same inputs give the same
  * bits.  Infinities: bf16 rows give what the formulas give; an infinite value of an fp32 tensor or of a factor, and in dA and dB of
  * any, may give NaN where they give an infinity.

@@ -62,6 +62,8 @@ __device__ __forceinline__ int find_rows(const LowrankArgs& a, int tile, int* s_
     for (int i = 0; i < IDS; ++i)
       if (id[i] >= 0) atomicAdd(&s_count[id[i]], 1);
     __syncthreads();
+  } else if (tile == 0) {
+    check_offsets(a.off, a.segments, a.n, a.check_word);
   }
   // one thread per segment: its tiles, added up
   const auto span = [&](int i) { return a.ids ? RowSpan{0, s_count[i]} : span_of(a.off, i, a.n); };
@@ -564,6 +566,7 @@ struct GradArgs {
   const float* scales;    // of dB
   const int32_t *off, *perm;
   float* part[2];         // [2 x runs][dim][rank]: shares of segments that several runs have
+  int* check_word;
   int n, G, rank, runs[2], blocks[2];
 };
 
@@ -670,8 +673,8 @@ __global__ void __launch_bounds__(LR_THREADS, GR_CTAS) lowrank_grad_kernel(GradA
 }
 
 // Joins the shares of segments that several runs have, in order, and clears the gradients of adapters without rows.  grid: (adapters,
-// pieces of a gradient, dB and dA); H: rows of a tile of the kernel in front.
-template <int H>
+// pieces of a gradient, dB and dA); H: rows of a tile of the kernel in front; CHECK: no kernel in front has looked at the offsets.
+template <int H, bool CHECK>
 __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
   __shared__ TileList list;
   const int tid = threadIdx.x, adapter = blockIdx.x, which = blockIdx.z;
@@ -679,6 +682,7 @@ __global__ void __launch_bounds__(LR_THREADS) lowrank_join_kernel(GradArgs a) {
   const TileRun run = list_tiles<H>(list, a.off, a.G, a.n, 0, a.runs[which]);
   pdl_wait();
   pdl_trigger();
+  if (CHECK && blockIdx.x == 0 && blockIdx.y == 0 && which == 0) check_offsets(a.off, a.G, a.n, a.check_word);
   if (!a.out[which]) return;
   const int first = list.first[adapter], end = list.first[adapter + 1], c0 = first / run.per, c1 = end > first ? (end - 1) / run.per : c0 - 1;
   if (c0 == c1) return;
@@ -809,13 +813,14 @@ cudaError_t launch_lowrank(const LowrankArgs& a, cudaStream_t st) {
   return by_rows(std::integral_constant<int, 4>());
 }
 
-cudaError_t launch_join(const GradArgs& a, bool stream, cudaStream_t st) {
+cudaError_t launch_join(const GradArgs& a, bool stream, bool check, cudaStream_t st) {
   const size_t dim = a.dim[0] > a.dim[1] ? a.dim[0] : a.dim[1], shares = (dim * a.rank / 4 + LR_THREADS - 1) / LR_THREADS;
   // CTAs of an adapter's gradient: few adapters share all SMs (8192 x 4096 -> 4096, one adapter, whole call 77/71 us)
   const size_t most = 2 * GPU_SMS / a.G > 32 ? 2 * GPU_SMS / a.G : 32;
   const dim3 grid(a.G, static_cast<unsigned>(shares < most ? shares : most), 2);
-  if (stream) return launch_chain(lowrank_join_kernel<STREAM_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
-  return launch_chain(lowrank_join_kernel<GR_ROWS>, grid, dim3(LR_THREADS), 0, st, a);
+  const auto go = [&](auto kernel) { return launch_chain(kernel, grid, dim3(LR_THREADS), 0, st, a); };
+  if (check) return stream ? go(lowrank_join_kernel<STREAM_ROWS, true>) : go(lowrank_join_kernel<GR_ROWS, true>);
+  return stream ? go(lowrank_join_kernel<STREAM_ROWS, false>) : go(lowrank_join_kernel<GR_ROWS, false>);
 }
 
 template <typename T>
@@ -858,7 +863,7 @@ cudaError_t launch_many(const LowrankArgs& a, bool back, const GradArgs* ga, cha
   cudaError_t e = cudaSuccess;
   if (s.factor || s.vec) e = launch_lowrank_stream(s, st);
   if (e != cudaSuccess || !vectors) return e;
-  SumArgs u = {planes, blocks_of(a.in_dim, stream_channels(a.rank)), vec, a.v, a.off, a.perm, a.n, a.G, a.rank, a.segments > a.G};
+  SumArgs u = {planes, blocks_of(a.in_dim, stream_channels(a.rank)), vec, a.v, a.off, a.perm, a.check_word, a.n, a.G, a.rank, a.segments > a.G};
   e = launch_lowrank_sum(u, st);
   if (e != cudaSuccess) return e;
   if (a.y) {
@@ -1045,6 +1050,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
   ga.scales = scales;
   ga.off = ids ? off_ws : off;
   ga.perm = ids ? perm : nullptr;
+  ga.check_word = a.check_word;
   ga.n = n;
   ga.G = desc->n_adapters;
   ga.rank = desc->rank;
@@ -1060,7 +1066,7 @@ int emoe_lowrank_backward(emoe_ctx* ctx, const emoe_lowrank_desc* desc, const vo
     if (dx || dA) EMOE_CALL(ctx, bf16 ? (launch_lowrank<__nv_bfloat16, true>(a, st)) : (launch_lowrank<float, true>(a, st)));
     if (dA || dB) EMOE_CALL(ctx, bf16 ? launch_grads<__nv_bfloat16>(ga, st) : launch_grads<float>(ga, st));
   }
-  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, streams, st));
+  if (dA || dB) EMOE_CALL(ctx, launch_join(ga, streams, off && !dx && !dA, st));
   return EMOE_OK;
 }
 

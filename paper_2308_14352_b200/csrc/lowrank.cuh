@@ -81,6 +81,14 @@ __device__ __forceinline__ RowSpan span_of(const int32_t* __restrict__ off, int 
   const int begin = min(max(off[i], 0), n), end = min(max(off[i + 1], 0), n);
   return {begin, max(end - begin, 0)};
 }
+// Offsets that descend or leave the rows set the check word: one CTA of a call looks at them, in the fused kernel, the sum of the vectors or (dB alone) the join,
+// which have registers to spare.
+__device__ __forceinline__ void check_offsets(const int32_t* __restrict__ off, int segments, int n, int* check_word) {
+  bool bad = false;
+#pragma unroll 1
+  for (int i = threadIdx.x; i < segments; i += blockDim.x) bad |= off[i] < 0 || off[i + 1] < off[i] || off[i + 1] > n;
+  if (bad) atomicOr(check_word, CHECK_BAD_EXPERT_ID);
+}
 
 // ---- rows shared out evenly ----------------------------------------------------------------------
 // The rows of every segment (the G adapters and, where there is one more, the rows of none) make tiles of H rows, the last of a
@@ -213,6 +221,7 @@ struct SumArgs {
   float* by_place;   // [n][rank]
   float* by_row;     // null: not wanted
   const int32_t *off, *perm;
+  int* check_word;
   int n, G, rank, with_none;  // with_none: the rows behind the last adapter's get zeros
 };
 cudaError_t launch_lowrank_sum(const SumArgs& a, cudaStream_t st);

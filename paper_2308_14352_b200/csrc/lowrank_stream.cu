@@ -425,6 +425,7 @@ __global__ void __launch_bounds__(SK_THREADS, 1) lowrank_stream_kernel(StreamArg
 __global__ void __launch_bounds__(256) lowrank_sum_kernel(SumArgs a) {
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x == 0) check_offsets(a.off, a.G, a.n, a.check_word);
   const int lanes = a.rank > 32 ? 16 : a.rank > 16 ? 8 : 4, place = blockIdx.x * (256 / lanes) + threadIdx.x / lanes, r = threadIdx.x % lanes * 4;
   if (place >= a.n || r >= a.rank) return;
   const bool mine = place >= a.off[0] && place < a.off[a.G];
@@ -512,7 +513,7 @@ __global__ void __launch_bounds__(UP_THREADS, 1) lowrank_up_kernel(UpArgs a) {
     wait_words[PIPE_FRONT] = 1;  // until the vectors' warps are past their wait for the kernel in front
   }
   TileRun run = list_tiles<STREAM_ROWS>(list, a.off, a.segments, a.n, blockIdx.x, a.runs);
-  run.hi = min(run.hi, run.lo + UP_RUN);  // (longer only where the segments overlap)
+  run.hi = min(run.hi, run.lo + UP_RUN);  // (longer only where the segments overlap, which the kernel in front has reported)
   if (run.lo >= run.hi) {
     pdl_wait();
     pdl_trigger();
