@@ -487,9 +487,11 @@ def emoe_rank_experts2(prior2_layer, prev2_ids, prev1_ids):
 
 # ---- rows in expert order, gates' gradient, low-rank adapters ----------------------------------
 # On small inputs these calls are shorter on the GPU than ctypes' own work per call, so they go through _pycall (csrc/pycall.cpp),
-# with the arguments' kinds from the declarations above.
+# with the arguments' kinds from the declarations above; through ctypes where it has not been built for this interpreter.
 
 _fast = None
+_TRAINING_CALLS = ("emoe_dispatch", "emoe_dispatch_backward", "emoe_combine", "emoe_combine_backward", "emoe_gate_backward",
+                   "emoe_lowrank_forward", "emoe_lowrank_backward")
 
 
 def _calls() -> SimpleNamespace:
@@ -498,12 +500,12 @@ def _calls() -> SimpleNamespace:
         L = lib()
         try:
             from . import _pycall
-        except ImportError as e:
-            raise RuntimeError("_pycall.so not found: build it with `python -m paper_2308_14352_b200.build`") from e
+        except ModuleNotFoundError:
+            _fast = SimpleNamespace(**{name: getattr(L, name) for name in _TRAINING_CALLS})
+            return _fast
         kind = {ctypes.c_void_p: "p", ctypes.c_int: "i"}
         bound = {}
-        for name in ("emoe_dispatch", "emoe_dispatch_backward", "emoe_combine", "emoe_combine_backward", "emoe_gate_backward",
-                     "emoe_lowrank_forward", "emoe_lowrank_backward"):
+        for name in _TRAINING_CALLS:
             f = getattr(L, name)
             descs = tuple(t._type_ for t in f.argtypes if t not in kind)
             bound[name] = _pycall.bind(ctypes.cast(f, ctypes.c_void_p).value, "".join(kind.get(t, "s") for t in f.argtypes), descs, L)
