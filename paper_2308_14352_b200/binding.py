@@ -184,15 +184,25 @@ def status_string(status: int) -> str:
     return lib().emoe_status_string(status).decode()
 
 
+_device_of = {}  # of the contexts that were made here
+
+
 def emoe_create(device: int, workspace_bytes: int) -> int:
     st = ctypes.c_int(0)
     ctx = lib().emoe_create(device, workspace_bytes, ctypes.byref(st))
     if not ctx:
         raise EmoeError(st.value, "emoe_create")
+    _device_of[ctx] = device
     return ctx
 
 
+def context_device(ctx: int) -> Optional[int]:
+    """The device that a context's calls run on; None for a handle that was not made here."""
+    return _device_of.get(ctx)
+
+
 def emoe_destroy(ctx: int) -> None:
+    _device_of.pop(ctx, None)
     _check(lib().emoe_destroy(ctx), "emoe_destroy")
 
 

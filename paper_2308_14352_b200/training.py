@@ -31,9 +31,11 @@ def _check(t: torch.Tensor, name: str, shape, dtype, device) -> torch.Tensor:
     return t
 
 
-def _gpu(device: torch.device, name: str) -> torch.device:
+def _gpu(ctx: int, device: torch.device, name: str) -> torch.device:
     if device.type != "cuda":
         raise ValueError(f"{name}: expected a tensor on a GPU, got one on {device}")
+    if B.context_device(ctx) not in (None, device.index):
+        raise ValueError(f"{name}: on {device}, but the context works on device {B.context_device(ctx)}")
     return device
 
 
@@ -54,7 +56,7 @@ class ExpertRows:
         self.token_dtype, self.row_dtype = token_dtype, row_dtype or token_dtype
         if self.token_dtype not in _CODE or self.row_dtype not in _CODE:
             raise ValueError("tokens and rows are float32 or bfloat16")
-        self.device = torch.device("cuda", device)
+        self.device = _gpu(ctx, torch.device("cuda", device), "rows")
         self.desc = B.emoe_dispatch_desc(d, n_experts, top_k, _CODE[self.token_dtype], _CODE[self.row_dtype], 0, 0, 0)
         self.tokens = 0  # of the last batch dispatched
 
@@ -126,7 +128,7 @@ def gate_backward(ctx: int, logits: torch.Tensor, ids: torch.Tensor, dgates: tor
     if logits.dim() != 2 or ids.dim() != 2:
         raise ValueError("logits are [tokens][experts], ids [tokens][picks]")
     T, E = logits.shape
-    _gpu(logits.device, "logits")
+    _gpu(ctx, logits.device, "logits")
     _check(logits, "logits", (T, E), torch.float32, logits.device)
     _check(ids, "ids", (T, ids.shape[1]), torch.int32, logits.device)
     _check(dgates, "dgates", ids.shape, torch.float32, logits.device)
@@ -142,7 +144,7 @@ class LowRankAdapters:
     def __init__(self, ctx: int, A: torch.Tensor, Bm: torch.Tensor, scales: Optional[torch.Tensor] = None):
         if A.dim() != 3 or Bm.dim() != 3 or A.dtype not in _CODE:
             raise ValueError("A is [adapters][rank][in], B [adapters][out][rank], float32 or bfloat16")
-        self.ctx, self.device, self.dtype = ctx, _gpu(A.device, "A"), A.dtype
+        self.ctx, self.device, self.dtype = ctx, _gpu(ctx, A.device, "A"), A.dtype
         self.n_adapters, self.rank, self.in_dim = A.shape
         self.out_dim = Bm.shape[1]
         self.A = _check(A, "A", A.shape, A.dtype, self.device)
