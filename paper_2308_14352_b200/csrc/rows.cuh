@@ -12,21 +12,22 @@ struct Piece {
   uint32_t w[WORDS];
 };
 
-// Reads that are used once (activations): not kept in L1.
+// Reads that are used once (activations): not kept in L1.  They stay in front of the stores behind them ("memory"): a row may be written where it was read.
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[8]) {
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-               : "l"(static_cast<const char*>(p) + 16));
+               : "l"(static_cast<const char*>(p) + 16)
+               : "memory");
 }
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[4]) {
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
 }
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[1]) {
-  asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(p) : "memory");
 }
 __device__ __forceinline__ void load_words(const void* p, uint32_t (&w)[2]) {
-  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p) : "memory");
 }
 template <typename T, int VEC>
 __device__ __forceinline__ Piece<T, VEC> load_piece(const T* p) {
