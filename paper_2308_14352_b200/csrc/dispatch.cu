@@ -82,7 +82,9 @@ __device__ __forceinline__ void write_dots(const RowsArgs& a, float (&dot)[KM], 
   }
 }
 
-constexpr int SPREAD_FIRST = 8 * GPU_SMS;  // CTAs of the first round
+// CTAs of the first round with one or two picks.  With more picks five of eight are resident while the sort runs, and the others pull their tokens just before
+// they read them.
+constexpr int SPREAD_FIRST = 8 * GPU_SMS;
 __device__ __forceinline__ void prefetch_l2(const void* p, int bytes) {  // both multiples of 16
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
 }

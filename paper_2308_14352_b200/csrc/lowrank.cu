@@ -12,7 +12,7 @@
 // Precision.  The tensor cores multiply bf16 exactly and add in fp32.  bf16 tensors enter as they are; an fp32 value enters as the
 // sum of bf16 parts: three (24 bits, the value itself) where the result is fp32, so that it has fp32's accuracy, two (16 bits) for the
 // low-rank vector of a bf16 result, whose own rounding is 2^-9.  Of the nine products of two values in three parts the three smallest
-// (2^-24 of the product) are left out.
+// are left out: with second parts below 2^-7 and third ones below 2^-15 they are 2^-21 of the product at most, 2^-24 on average.
 #include <cooperative_groups.h>
 
 #include "lowrank.cuh"
@@ -716,9 +716,14 @@ int runs_for(int n, int segments, int blocks, int slots, int tile, int most) {
   return runs < tiles ? runs : tiles;
 }
 // Which bf16 calls take the streaming kernels, by the bytes of the rows read and written: they (and their launches) cost some 10 us more at the
-// start and run at the speed of memory from there on.  us, fused / streaming, 4096 -> 4096.  Forward, rank 16: 2048 rows 15.9/20.6 (4099 rows,
-// 4096 -> 14336, rank 32: 148/73); rank 64: 1024 rows 25/35, 1536 rows 35/32.  Backward, rank 16: 512 rows 29.6/30.5, 1024 rows 41/29
-// (1024 -> 1024: 2048 rows 21/24, 4096 rows 31/28); rank 64: 256 rows 59/63, 512 rows 75/66.
+// start and gain from there on.  The fused kernel's time goes in steps, by rounds of clusters, so that near the limits either may be the faster one, by a
+// fifth at most.  us, fused / streaming, 8 adapters with ids (in brackets 16 by offsets):
+//   forward, 4096 -> 4096   rank 16: 2048 rows 22/32 (27/24), 3200 rows 35/33 (29/26), 4557 rows 35/40 (40/34), 6000 rows 49/43 (44/36),
+//                           8192 rows 55/53 (49/45); rank 32: 4557 rows 38/44 (49/38); rank 64: 1024 rows 24/34 (24/26),
+//                           1300 rows (33/28), 1536 rows 38/33 (34/29)
+//           2048 -> 2048    rank 16: 9114 rows 35/39 (28/32), 12000 rows 51/44;  4096 -> 14336, rank 32: 2000 rows (42/45), 4099 rows (74/66)
+//   backward, 4096 -> 4096  rank 16: 512 rows 28/29 (24/26), 1100 rows 45/38 (1024: 40/29); rank 64: 256 rows (48/48), 384 rows 44/38 (51/49)
+//           1024 -> 1024    rank 16: 2048 rows 27/31 (23/23), 4096 rows (27/27);  2048 -> 2048: 1342 rows 32/31 (24/25)
 bool takes_stream(const emoe_lowrank_desc& D, int n, bool back) {
   const double K = D.in_dim, N = D.out_dim, bytes = 2.0 * n * (back ? 3 * K + N : K + 2 * N);
   return D.dtype == EMOE_DTYPE_BF16 && bytes > (back ? (D.rank > 32 ? 12e6 : 20e6) : (D.rank > 32 ? 32e6 : 80e6));

@@ -3,7 +3,9 @@ order and back, the gates' gradient, low-rank adapters.  As in ``layer``, PyTorc
 computation is a call into libemoe.  Tensors are checked here (type, shape, device), since the library sees addresses only.
 Calls go to the stream that torch works on at the time, whose memory their results are; a caller that names another stream orders the two.
 
-One step of a layer with an adapter per expert, its packed experts frozen:
+One step of a layer with an adapter per expert, its experts frozen.  expert_outputs and through_experts are the experts' own products, forward and
+back, in expert order: the program's, from experts that it holds unpacked (for packed ones there is no gradient call, and emoe_moe_forward gives the
+gate-weighted sum alone):
 
     rows = er.dispatch(x, ids)                                       # expert order; er.off: first row of each expert
     out = ad.forward(rows, base=expert_outputs, off=er.off, keep=True)
