@@ -259,11 +259,13 @@ int emoe_gate_backward(emoe_ctx* ctx, const float* logits, int T, int E, const i
  * Rows of no adapter: with ids y = base and v = 0 (nothing is touched where y is base), with off they are left as they were; they
  * take no part in dA and dB.  An id other than -1 outside [0,n_adapters) counts as -1 and sets the device check word.
  * Offsets that descend or lie outside 0 .. n set it too; the results of such a call are undefined, but nothing outside its tensors is touched.
- * Precision: sums are held in fp32.  Tensor cores make most of the additions, and cut where a rounded sum would round: v, dA and dB are
- * off by 1e-7 to 7e-7 of their norm, y and dx of fp32 tensors by up to 4e-7 (measured; the most for sums over 512 channels and 1024 rows).  fp32 values enter as three
- * bf16 parts, all their 24 bits; of the nine products of two values the three smallest are left out, 2^-24 of the product on average and
- * 2^-21 at most.  In bf16 results, rounded once, the low-rank vector has 16 bits.  The same inputs give the same bits.  Infinities: bf16 rows give what the formulas give; an infinite value of an fp32 tensor or of a factor, and in dA and dB of
- * any, may give NaN where they give an infinity.
+ * Precision: sums are held in fp32.  Tensor cores make most of the additions, and cut where a rounded sum would round: v, dA and dB
+ * are off by 1e-7 to 7e-7 of their norm, y and dx of fp32 tensors by up to 4e-7 (measured; the most for sums over 512 channels and
+ * 1024 rows).  fp32 values enter as three bf16 parts, all their 24 bits; of the nine products of two values the three smallest are left
+ * out, 2^-24 of the product on average and 2^-21 at most.  In bf16 results, rounded once, the low-rank vector has 16 bits.  The same inputs
+ * give the same bits.
+ * Infinities: bf16 rows give what the formulas give; an infinite value of an fp32 tensor or of a factor, and in dA and dB of any, may give
+ * NaN where they give an infinity.
  * Limits: rank 1 .. EMOE_MAX_RANK (any; multiples of 8 are faster), in_dim and out_dim multiples of 8 and at most 8388352, strides multiples of
  * 16 bytes, tensors 16-byte aligned, n < 2^27. */
 typedef struct emoe_lowrank_desc {
